@@ -214,6 +214,97 @@ int trispec_kv_paged_bytes(const trispec_model *m, int32_t n_pages, size_t *byte
 int trispec_kv_create_paged(const trispec_model *m, void *k_pool_dev, void *v_pool_dev, const int32_t *page_table_dev,
                             int32_t batch, int32_t max_pages_per_seq, int32_t n_pages, trispec_kv **out);
 
+/*
+ * The cache held in 4 bits.  Blocks of 32 features of one head of one slot share a scale 2^(byte - 127); an element is a sign and
+ * one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (the MXFP4 format of the OCP microscaling specification): 4.25 bits an element, 0.27 of bf16.
+ * A row is quantised as it is written, every block by itself: byte = the exponent that leaves the largest magnitude below 7 times
+ * the scale (at most 252), elements rounded to nearest, ties to the even code, cut off at 6.  A block that holds an infinity
+ * or a NaN gets byte 255 and reads back as NaN whole.  Values read back are exact in bf16.
+ *
+ * ONE LAYER of it, S = slots of a block of memory (a sequence: capacity; a page: TRISPEC_KV_PAGE), block = sequence or page:
+ *   k_codes  [block][n_kv_heads][S][head_dim / 2]            two features a byte, the even one in the low half
+ *   k_scales [block][n_kv_heads][S][head_dim / 32]
+ *   v_codes  [block][n_kv_heads][S / 8][head_dim / 4][8][2]  of slot 8 i + j: entry j of group i; two bytes = four features
+ *   v_scales [block][n_kv_heads][S / 8][head_dim / 32][8]
+ * all device memory, 16-byte aligned, of the sizes that trispec_mx_cache_bytes gives.  Contiguous: page_table NULL, capacity a
+ * multiple of 64.  Paged: page_table as in trispec_kv_create_paged (entries outside the pool are clamped into it), capacity =
+ * max_pages * TRISPEC_KV_PAGE whatever the field says.  head_dim 64 or 128, batch up to TRISPEC_MAX_BATCH.
+ */
+typedef struct {
+  void *k_codes, *k_scales, *v_codes, *v_scales;
+  const int32_t *page_table;   /* device [batch][max_pages], or NULL */
+  int32_t batch, n_kv_heads, head_dim;
+  int32_t capacity;            /* slots of a sequence */
+  int32_t max_pages, n_pages;  /* paged only */
+} trispec_mx_cache;
+
+/* Rows of one tensor on the device: element (sequence b, row i, head h, feature f) is
+ * data[b * seq_stride + i * row_stride + h * head_dim + f].  data 16-byte aligned, strides multiples of 16 bytes. */
+typedef struct {
+  void *data;
+  int64_t row_stride, seq_stride;   /* elements; >= 0 */
+} trispec_mx_rows;
+
+/* Bytes of k_codes (= of v_codes) and of k_scales (= of v_scales) of one layer.  Reads the sizes of *c only.
+ * Errors: TRISPEC_ENULL, TRISPEC_ENODES (batch), TRISPEC_ESHAPE (heads, head_dim), TRISPEC_ECAPACITY. */
+int trispec_mx_cache_bytes(const trispec_mx_cache *c, size_t *code_bytes, size_t *scale_bytes);
+
+/* Writes rows into the cache, quantised: row i < count[b] of sequence b goes to slot start[b] + i.  Slots outside that range keep
+ * their bytes, the neighbours in a group of 8 too.  k, v: [batch][count][n_kv_heads * head_dim] of dtype (TRISPEC_F32 |
+ * TRISPEC_BF16), keys after the rotary embedding.  start_host, count_host: HOST [batch]; a count of 0 writes nothing.
+ * One launch on `stream`, nothing else: calls on one stream see each other's rows in order.
+ * Two sequences must not share a page that a call writes.
+ * Errors: those of trispec_mx_cache_bytes, TRISPEC_ECAPACITY (a negative start or count, or an end beyond the capacity),
+ * TRISPEC_EARG (dtype, alignment, strides), TRISPEC_ELAUNCH. */
+int trispec_mx_append(const trispec_mx_cache *c, const trispec_mx_rows *k, const trispec_mx_rows *v, int32_t dtype,
+                      const int32_t *start_host, const int32_t *count_host, void *stream);
+
+/* Reads slots start[b] .. start[b] + count[b] of every sequence back into rows 0 .. count[b] of k and v (either may be NULL), in
+ * dtype; rows behind a sequence's count are left as they are.  What a slot holds that was never written is unspecified.
+ * Errors: those of trispec_mx_append; TRISPEC_EARG also where rows of the outputs overlap. */
+int trispec_mx_read(const trispec_mx_cache *c, const trispec_mx_rows *k, const trispec_mx_rows *v, int32_t dtype,
+                    const int32_t *start_host, const int32_t *count_host, void *stream);
+
+/*
+ * Grouped-query attention of n_nodes nodes of every sequence over the first ctx_len[b] slots of the cache and the
+ * nodes on each one's root path (itself included), as in a layer of trispec_verify: softmax(q . K / sqrt(head_dim)) V, the context's K
+ * and V as they read back, the nodes' own as they are given.  One node is plain decoding.
+ *   q             [batch][n_nodes][n_q_heads * head_dim], rotated;  k, v [batch][n_nodes][n_kv_heads * head_dim].  data NULL in both k and v:
+ *                 the nodes see the cache alone, and a node that sees no key gets zeros
+ *   dtype         of q, k, v and out.  TRISPEC_F32: operands as bf16 high + low pairs; TRISPEC_BF16: exact queries, probabilities
+ *                 rounded to bf16.  Sums, maxima and the nodes' own part are fp32 either way
+ *   tree_parents  HOST [batch][n_nodes] as in trispec_verify, or NULL: a chain
+ *   append        1: the nodes' k and v are also written to slots ctx_len[b] + i (trispec_mx_append, in the same launch)
+ *   out           [batch * n_nodes] rows of n_q_heads * head_dim, out_row_stride elements apart
+ *   workspace     device, 256-byte aligned, trispec_mx_attend_workspace_bytes() bytes; calls that may overlap in time (two streams, two
+ *                 captured graphs) need one each
+ * ctx_len_host: HOST [batch], read at the call (a captured call replays with the lengths it was captured with).
+ * Limits as trispec_verify: batch * n_nodes <= TRISPEC_MAX_ROWS, at most 8 query heads per kv head, n_q_heads / n_kv_heads * n_nodes <= 512.
+ * Two launches on `stream`; no allocation, no synchronisation.
+ * Errors: those of trispec_mx_append, TRISPEC_ENULL, TRISPEC_ESHAPE, TRISPEC_ENODES, TRISPEC_ETREE, TRISPEC_EWORKSPACE.
+ */
+typedef struct {
+  trispec_mx_rows q, k, v;
+  int32_t dtype, n_nodes, n_q_heads;
+  const int32_t *tree_parents;
+  int32_t append;
+  void *out;
+  int64_t out_row_stride;
+  void *workspace;
+  size_t workspace_bytes;
+  void *stream;
+} trispec_mx_attend_args;
+int trispec_mx_attend_workspace_bytes(int32_t batch, int32_t n_nodes, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                      size_t *bytes);
+int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, const trispec_mx_attend_args *a);
+
+/* A cache object over such memory, for bf16 models: every other call takes it like a bf16 one (trispec_verify, trispec_kv_commit,
+ * trispec_ternary_*).  `c` describes layer 0; each array holds the model's n_layers layers one behind another.  A pass quantises the
+ * draft nodes' rows as it stores them and attends over the context as it reads back; the nodes of the pass see each other unrounded, as with
+ * a bf16 cache.  Errors: TRISPEC_ENULL, TRISPEC_EMISMATCH (n_kv_heads or head_dim are not the model's), TRISPEC_ESHAPE (an fp32
+ * model), those of trispec_mx_cache_bytes, TRISPEC_EARG (alignment). */
+int trispec_kv_create_mx(const trispec_model *m, const trispec_mx_cache *c, trispec_kv **out);
+
 /* The context lengths a cache object holds now (they grow with trispec_kv_commit).
  *   ctx_len_host  HOST [batch], written.   Errors: TRISPEC_ENULL. */
 int trispec_kv_get_len(const trispec_kv *kv, int32_t *ctx_len_host);

@@ -8,6 +8,7 @@ the binding's entry points raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Callable, Dict, List, Optional, Sequence
 
@@ -33,6 +34,8 @@ EXPORTS = [
     "trispec_prune_reroot", "trispec_draft_ranks", "trispec_pack_matrix_bytes", "trispec_pack_matrix",
     "trispec_kv_get_len", "trispec_kv_paged_bytes", "trispec_kv_create_paged", "trispec_ternary_create", "trispec_ternary_destroy", "trispec_ternary_start",
     "trispec_ternary_resume", "trispec_ternary_round", "trispec_ternary_sequence", "trispec_ternary_round_sample",
+    "trispec_mx_cache_bytes", "trispec_mx_append", "trispec_mx_read", "trispec_mx_attend_workspace_bytes", "trispec_mx_attend",
+    "trispec_kv_create_mx",
 ]
 K_GEMM, K_HEAD, K_ATTN = 0, 1, 2
 LAUNCH_PER_MATMUL, LAUNCH_PER_LAYER = 0, 1
@@ -100,6 +103,22 @@ class SampleOpts(C.Structure):
                 ("n_forced", C.c_int32), ("p_draft", C.c_void_p), ("u_accept", C.c_void_p),
                 ("u_sample", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t),
                 ("stream", C.c_void_p)]
+
+
+class MXCacheDesc(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales", "page_table")] + \
+               [(n, C.c_int32) for n in ("batch", "n_kv_heads", "head_dim", "capacity", "max_pages", "n_pages")]
+
+
+class MXRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("seq_stride", C.c_int64)]
+
+
+class MXAttendArgs(C.Structure):
+    _fields_ = [("q", MXRows), ("k", MXRows), ("v", MXRows), ("dtype", C.c_int32), ("n_nodes", C.c_int32),
+                ("n_q_heads", C.c_int32), ("tree_parents", C.POINTER(C.c_int32)), ("append", C.c_int32),
+                ("out", C.c_void_p), ("out_row_stride", C.c_int64), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
 
 
 class TriSpecError(RuntimeError):
@@ -176,6 +195,13 @@ def lib() -> C.CDLL:
         l.trispec_timer_read.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_double),
                                          C.POINTER(C.c_double)]
         l.trispec_timer_destroy.argtypes = [C.c_void_p]
+        _pc, _pr = C.POINTER(MXCacheDesc), C.POINTER(MXRows)
+        l.trispec_mx_cache_bytes.argtypes = [_pc, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+        l.trispec_mx_append.argtypes = [_pc, _pr, _pr, C.c_int32, _pi, _pi, C.c_void_p]
+        l.trispec_mx_read.argtypes = l.trispec_mx_append.argtypes
+        l.trispec_mx_attend_workspace_bytes.argtypes = [C.c_int32] * 5 + [C.POINTER(C.c_size_t)]
+        l.trispec_mx_attend.argtypes = [_pc, _pi, C.POINTER(MXAttendArgs)]
+        l.trispec_kv_create_mx.argtypes = [C.c_void_p, _pc, C.POINTER(C.c_void_p)]
         _lib = l
     return _lib
 
@@ -280,7 +306,7 @@ class KVCache:
                                                       dtype=dt, device=device)
         assert self.k.is_contiguous() and self.v.is_contiguous()
         assert self.k.numel() * self.k.element_size() == n.value == self.v.numel() * self.v.element_size()
-        self.model, self.batch, self.capacity = model, batch, capacity
+        self.model, self.batch, self.capacity, self.device = model, batch, capacity, self.k.device
         self.handle = C.c_void_p()
         check(lib().trispec_kv_create(model.handle, self.k.data_ptr(), self.v.data_ptr(), batch, capacity,
                                       C.byref(self.handle)))
@@ -335,6 +361,18 @@ class KVCache:
 KV_PAGE = 256
 
 
+def _page_table(batch: int, max_pages: int, table, spare_pages: int, seed: int, device):
+    """(device table [batch, max_pages], pages of the pool): the given table, or a seeded shuffle with some pages left unmapped."""
+    if table is None:
+        n_pages = batch * max_pages + spare_pages
+        g = torch.Generator().manual_seed(seed)
+        table = torch.randperm(n_pages, generator=g)[: batch * max_pages].reshape(batch, max_pages)
+    else:
+        table = torch.as_tensor(table).reshape(batch, max_pages)
+        n_pages = int(table.max()) + 1 + spare_pages
+    return table.to(torch.int32).to(device).contiguous(), n_pages
+
+
 class PagedKVCache(KVCache):
     """trispec_kv over two page pools and a device page table (trispec_kv_create_paged):
     K pool [L, n_pages, n_kv, KV_PAGE, d], V pool [L, n_pages, n_kv, d, KV_PAGE]; slot s of sequence b is
@@ -346,21 +384,14 @@ class PagedKVCache(KVCache):
                  device="cuda"):
         c = model.cfg
         self.max_pages = (capacity + KV_PAGE - 1) // KV_PAGE
-        if table is None:
-            self.n_pages = batch * self.max_pages + spare_pages
-            g = torch.Generator().manual_seed(seed)
-            table = torch.randperm(self.n_pages, generator=g)[: batch * self.max_pages].reshape(batch, self.max_pages)
-        else:
-            table = torch.as_tensor(table).reshape(batch, self.max_pages)
-            self.n_pages = int(table.max()) + 1 + spare_pages
-        self.table = table.to(torch.int32).to(device).contiguous()
+        self.table, self.n_pages = _page_table(batch, self.max_pages, table, spare_pages, seed, device)
         n = C.c_size_t()
         check(lib().trispec_kv_paged_bytes(model.handle, self.n_pages, C.byref(n)))
         dt = _torch_dtype(c.dtype)
         self.k_pool = torch.zeros((c.n_layers, self.n_pages, c.n_kv_heads, KV_PAGE, c.head_dim), dtype=dt, device=device)
         self.v_pool = torch.zeros((c.n_layers, self.n_pages, c.n_kv_heads, c.head_dim, KV_PAGE), dtype=dt, device=device)
         assert self.k_pool.numel() * self.k_pool.element_size() == n.value
-        self.model, self.batch, self.capacity = model, batch, self.max_pages * KV_PAGE
+        self.model, self.batch, self.capacity, self.device = model, batch, self.max_pages * KV_PAGE, self.table.device
         self.handle = C.c_void_p()
         check(lib().trispec_kv_create_paged(model.handle, self.k_pool.data_ptr(), self.v_pool.data_ptr(),
                                             self.table.data_ptr(), batch, self.max_pages, self.n_pages,
@@ -397,6 +428,192 @@ class PagedKVCache(KVCache):
             pages = self.table[:, p0 // KV_PAGE].long()                                  # [B]
             self.k_pool[layer, pages, :, :n, :] = k[:, :, p0:p0 + n, :].to(self.k_pool.dtype)
             self.v_pool[layer, pages, :, :, :n] = v[:, :, p0:p0 + n, :].to(self.v_pool.dtype).transpose(-1, -2)
+
+
+class MXCache:
+    """One layer of the cache held in 4 bits (trispec_mx_cache) over tensors the caller supplies, all uint8, contiguous:
+    k_codes  [blocks, n_kv, S, d / 2]         k_scales [blocks, n_kv, S, d / 32]
+    v_codes  [blocks, n_kv, S / 8, d / 4, 8, 2]  v_scales [blocks, n_kv, S / 8, d / 32, 8]
+    with a block per sequence, S slots each, or, with `table` (int32 [batch, max_pages] on the device), pages of S = KV_PAGE slots.
+    The object keeps them alive."""
+
+    def __init__(self, k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor,
+                 table: Optional[torch.Tensor] = None):
+        blocks, n_kv, slots, half = k_codes.shape
+        d = 2 * half
+        for t, shape in ((k_codes, (blocks, n_kv, slots, half)), (k_scales, (blocks, n_kv, slots, d // 32)),
+                         (v_codes, (blocks, n_kv, slots // 8, d // 4, 8, 2)), (v_scales, (blocks, n_kv, slots // 8, d // 32, 8))):
+            if t.dtype != torch.uint8 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != k_codes.device:
+                raise ValueError(f"MXCache: a uint8 tensor of {shape}, contiguous and on one device, is wanted")
+        if table is not None and (table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous()
+                                  or table.device != k_codes.device or slots != KV_PAGE):
+            raise ValueError("MXCache: pages of KV_PAGE slots behind an int32 table [batch, max_pages] on the same device are wanted")
+        self.tensors = (k_codes, k_scales, v_codes, v_scales, table)
+        self.device, self.n_kv_heads, self.head_dim = k_codes.device, n_kv, d
+        self.batch, max_pages = (blocks, 0) if table is None else table.shape
+        self.capacity = slots if table is None else max_pages * KV_PAGE
+        self.desc = MXCacheDesc(*[t.data_ptr() for t in self.tensors[:4]], None if table is None else table.data_ptr(),
+                                self.batch, n_kv, d, self.capacity, max_pages, 0 if table is None else blocks)
+        a, b = C.c_size_t(), C.c_size_t()
+        check(lib().trispec_mx_cache_bytes(C.byref(self.desc), C.byref(a), C.byref(b)))
+        assert a.value == k_codes.numel() == v_codes.numel() and b.value == k_scales.numel() == v_scales.numel()
+        self.ref = C.byref(self.desc)
+        self._workspace_bytes: Dict[tuple, int] = {}
+
+    @classmethod
+    def empty(cls, batch: int, n_kv_heads: int, head_dim: int, capacity: int, table: Optional[torch.Tensor] = None,
+              n_pages: Optional[int] = None, device="cuda") -> "MXCache":
+        """Zeroed buffers: `capacity` slots a sequence, or `n_pages` pages behind `table`."""
+        blocks, slots = (batch, capacity) if table is None else (n_pages, KV_PAGE)
+        u8 = dict(dtype=torch.uint8, device=device)
+        return cls(torch.zeros((blocks, n_kv_heads, slots, head_dim // 2), **u8),
+                   torch.zeros((blocks, n_kv_heads, slots, head_dim // 32), **u8),
+                   torch.zeros((blocks, n_kv_heads, slots // 8, head_dim // 4, 8, 2), **u8),
+                   torch.zeros((blocks, n_kv_heads, slots // 8, head_dim // 32, 8), **u8), table)
+
+    def rows(self, t: torch.Tensor, n_heads: int, dtype: torch.dtype) -> MXRows:
+        if (t.dim() != 4 or t.shape[0] != self.batch or t.shape[2] != n_heads or t.shape[3] != self.head_dim or t.dtype != dtype
+                or t.device != self.device or t.stride(3) != 1 or (n_heads > 1 and t.stride(2) != self.head_dim)):
+            raise ValueError(f"a {dtype} tensor [{self.batch}, n, {n_heads}, {self.head_dim}] on {self.device} is wanted, the heads of a row side by side")
+        return MXRows(t.data_ptr(), t.stride(1), t.stride(0))
+
+    def ints(self, v: Sequence[int]):
+        if len(v) != self.batch:
+            raise ValueError(f"a number for each of the {self.batch} sequences is wanted")
+        return (C.c_int32 * self.batch)(*v)
+
+    def workspace_bytes(self, n_nodes: int, n_q_heads: int) -> int:
+        key = (n_nodes, n_q_heads)
+        if key not in self._workspace_bytes:
+            n = C.c_size_t()
+            check(lib().trispec_mx_attend_workspace_bytes(self.batch, n_nodes, n_q_heads, self.n_kv_heads, self.head_dim, C.byref(n)))
+            self._workspace_bytes[key] = n.value
+        return self._workspace_bytes[key]
+
+
+_MX_DTYPES = {torch.float32: TRISPEC_F32, torch.bfloat16: TRISPEC_BF16}
+
+
+def _mx_dtype(t: torch.dtype) -> int:
+    if t not in _MX_DTYPES:
+        raise ValueError("float32 or bfloat16 rows are wanted")
+    return _MX_DTYPES[t]
+
+
+def _on_device(fn):
+    """Runs an operator with the cache's device current: allocations, the stream and the launch are its."""
+    @functools.wraps(fn)
+    def call(cache, *args, stream=None, **kw):
+        if stream is None and cache.device.index == torch.cuda.current_device():
+            return fn(cache, *args, stream=torch.cuda.current_stream().cuda_stream, **kw)
+        with torch.cuda.device(cache.device), torch.cuda.stream(stream):   # what is allocated here belongs to that stream
+            return fn(cache, *args, stream=torch.cuda.current_stream().cuda_stream, **kw)
+    return call
+
+
+@_on_device
+def mx_append(cache: MXCache, k: torch.Tensor, v: torch.Tensor, start: Sequence[int], count: Optional[Sequence[int]] = None,
+              stream=None) -> None:
+    """trispec_mx_append: rows i < count[b] (default: all) of k and v [batch, n, n_kv, d] into slots start[b] + i."""
+    kr, vr = cache.rows(k, cache.n_kv_heads, k.dtype), cache.rows(v, cache.n_kv_heads, k.dtype)
+    n = k.shape[1]
+    if v.shape[1] != n or (count is not None and max(count, default=0) > n):
+        raise ValueError("mx_append: more rows are to be written than k and v hold")
+    check(lib().trispec_mx_append(cache.ref, C.byref(kr), C.byref(vr), _mx_dtype(k.dtype), cache.ints(start),
+                                  cache.ints([n] * cache.batch if count is None else count), stream))
+
+
+@_on_device
+def mx_read(cache: MXCache, start: Sequence[int], n: int, dtype: torch.dtype = torch.bfloat16, stream=None):
+    """trispec_mx_read: (k, v) [batch, n, n_kv, d] of the slots start[b] .. start[b] + n."""
+    k, v = torch.empty((2, cache.batch, n, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=cache.device)
+    row = cache.n_kv_heads * cache.head_dim
+    if n > 0:
+        kr, vr = MXRows(k.data_ptr(), row, n * row), MXRows(v.data_ptr(), row, n * row)
+        check(lib().trispec_mx_read(cache.ref, C.byref(kr), C.byref(vr), _mx_dtype(dtype), cache.ints(start), cache.ints([n] * cache.batch), stream))
+    return k, v
+
+
+@_on_device
+def mx_attend(cache: MXCache, ctx_len: Sequence[int], q: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+              parents: Optional[np.ndarray] = None, append: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """trispec_mx_attend: q [batch, n_nodes, n_q, d], k and v [batch, n_nodes, n_kv, d] (None: the cache alone), parents host int32
+    [batch, n_nodes] (None: a chain).  Returns [batch, n_nodes, n_q, d] in q's dtype.  `workspace`: uint8, at least
+    cache.workspace_bytes(n_nodes, n_q) long and 256-byte aligned; by default one is taken from torch's allocator."""
+    if q.dim() != 4:
+        raise ValueError("mx_attend: q [batch, n_nodes, n_q, d] is wanted")
+    b, m, heads, d = q.shape
+    a = MXAttendArgs()
+    a.q = cache.rows(q, heads, q.dtype)
+    if (k is None) != (v is None) or (k is not None and (k.shape[1] != m or v.shape[1] != m)):
+        raise ValueError("mx_attend: keys and values of all nodes, or of none, are wanted")
+    if k is not None:
+        a.k, a.v = cache.rows(k, cache.n_kv_heads, q.dtype), cache.rows(v, cache.n_kv_heads, q.dtype)
+    if parents is not None:
+        parents = np.ascontiguousarray(parents, dtype=np.int32)
+        if parents.shape != (b, m):
+            raise ValueError("mx_attend: a parent for each node is wanted")
+        a.tree_parents = parents.ctypes.data_as(C.POINTER(C.c_int32))
+    a.dtype, a.n_nodes, a.n_q_heads, a.append = _mx_dtype(q.dtype), m, heads, int(append)
+    need = cache.workspace_bytes(m, heads)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+    elif workspace.device != cache.device or not workspace.is_contiguous():
+        raise ValueError("mx_attend: a contiguous workspace on the cache's device is wanted")
+    out = torch.empty((b, m, heads, d), dtype=q.dtype, device=cache.device)
+    a.out, a.out_row_stride = out.data_ptr(), heads * d
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    a.stream = stream
+    check(lib().trispec_mx_attend(cache.ref, cache.ints(ctx_len), C.byref(a)))
+    return out
+
+
+class MXKVCache(KVCache):
+    """trispec_kv held in 4 bits (trispec_kv_create_mx), for bf16 models: all layers of the MXCache layout, contiguous or, with `paged`,
+    in pages behind a table as PagedKVCache makes it.  `k` and `v` READ the cache as dense bf16 tensors in KVCache's layout (copies);
+    write_layer and load_dense quantise into it."""
+
+    def __init__(self, model: Model, batch: int, capacity: int, paged: bool = False, table=None, spare_pages: int = 3, seed: int = 0,
+                 device="cuda"):
+        c = model.cfg
+        self.table = None
+        if paged or table is not None:
+            max_pages = (capacity + KV_PAGE - 1) // KV_PAGE
+            self.table, n_pages = _page_table(batch, max_pages, table, spare_pages, seed, device)
+            blocks, slots = n_pages, KV_PAGE
+        else:
+            blocks, slots = batch, capacity
+        u8 = dict(dtype=torch.uint8, device=device)
+        L, H, d = c.n_layers, c.n_kv_heads, c.head_dim
+        self.pools = (torch.zeros((L, blocks, H, slots, d // 2), **u8), torch.zeros((L, blocks, H, slots, d // 32), **u8),
+                      torch.zeros((L, blocks, H, slots // 8, d // 4, 8, 2), **u8), torch.zeros((L, blocks, H, slots // 8, d // 32, 8), **u8))
+        self.layers = [MXCache(*[p[l] for p in self.pools], self.table) for l in range(L)]
+        self.model, self.batch, self.capacity, self.device = model, batch, self.layers[0].capacity, self.layers[0].device
+        self.handle = C.c_void_p()
+        check(lib().trispec_kv_create_mx(model.handle, self.layers[0].ref, C.byref(self.handle)))
+        self.ctx_len = [0] * batch
+
+    def _dense(self, which: int) -> torch.Tensor:      # [L, B, n_kv, capacity, d]
+        return torch.stack([mx_read(c, [0] * self.batch, self.capacity)[which].transpose(1, 2) for c in self.layers])
+
+    @property
+    def k(self) -> torch.Tensor:          # [L, B, n_kv, capacity, d]
+        return self._dense(0)
+
+    @property
+    def v(self) -> torch.Tensor:          # [L, B, n_kv, d, capacity]
+        return self._dense(1).transpose(-1, -2)
+
+    def load_dense(self, k: torch.Tensor, v: torch.Tensor) -> None:
+        """k [L, B, n_kv, capacity, d], v [L, B, n_kv, d, capacity], quantised."""
+        for l in range(len(self.layers)):
+            self.write_layer(l, k[l], v[l].transpose(-1, -2))
+
+    def write_layer(self, layer: int, k: torch.Tensor, v: torch.Tensor) -> None:
+        """The first C slots of one layer: k, v [B, n_kv, C, d], quantised as they are."""
+        k, v = (t if t.dtype in _MX_DTYPES else t.float() for t in (k, v))
+        v = v.to(k.dtype)
+        mx_append(self.layers[layer], k.transpose(1, 2).contiguous(), v.transpose(1, 2).contiguous(), [0] * self.batch)
 
 
 class KernelTimer:

@@ -542,7 +542,28 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
   at.ctx = ctx;
   at.batch = B; at.n_nodes = n_nodes; at.n_q_heads = c.n_q_heads; at.n_kv_heads = c.n_kv_heads;
   at.head_dim = c.head_dim; at.kv = kv->map();
-  if (!f32) {
+  MxAttnArgs mx;
+  memset(&mx, 0, sizeof(mx));
+  if (kv->held_in_mx) {
+    const MxPlan p = plan_mx(B, c.n_kv_heads, group, n_nodes, true, max_keys);
+    const float *rows_f32 = (const float *)(ws + L.qkv_f32);
+    const int64_t seq = (int64_t)n_nodes * nqkv;
+    mx.ctx = ctx;
+    mx.q = {rows_f32, nqkv, seq};
+    mx.k = {rows_f32 + qd, nqkv, seq};
+    mx.v = {rows_f32 + qd + kvd, nqkv, seq};
+    mx.anc = at.anc;
+    mx.batch = B; mx.n_nodes = n_nodes; mx.n_q_heads = c.n_q_heads; mx.group = group; mx.head_dim = c.head_dim;
+    mx.dtype = TRISPEC_F32;
+    mx.append = 1;
+    mx.row_blocks = p.row_blocks; mx.row_waves = p.row_waves; mx.n_row_groups = p.n_row_groups;
+    mx.keys_per_split = p.keys_per_split; mx.n_splits = p.n_splits; mx.n_draft = p.n_draft;
+    mx.part_o = (float *)(ws + L.attn_o);
+    mx.part_m = (float *)(ws + L.attn_m);
+    mx.part_l = (float *)(ws + L.attn_l);
+    mx.out = attn_out;
+    mx.out_panel = (size_t)(rp / 32);
+  } else if (!f32) {
     const AttnPlan p = plan_attn(B, c.n_kv_heads, group, c.head_dim, n_nodes, tree_depth(tab, rows, n_nodes), max_keys, kv->page_table != nullptr);
     at.few = p.few;
     at.rows_per_wg = p.rows_per_wg; at.n_row_groups = p.n_row_groups;
@@ -554,12 +575,18 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
   at.part_l = (float *)(ws + L.attn_l);
   at.out = attn_out;
   at.out_panel = (size_t)(rp / 32);   // operand layout: number of 32-row blocks
-  auto attention = [&](char *kl, char *vl) {
-    at.k_cache = kl;
-    at.v_cache = vl;
+  auto attention = [&](int l) {
     double kvb = 0;
-    for (int b = 0; b < B; ++b) kvb += 2.0 * (kv->ctx_len[b] + n_nodes) * kvd * es;
+    const double element = kv->held_in_mx ? 0.5 + 1.0 / kMxBlock : (double)es;
+    for (int b = 0; b < B; ++b) kvb += 2.0 * (kv->ctx_len[b] + n_nodes) * kvd * element;
     TimedLaunch tl(opts->timer, TRISPEC_K_ATTN, st, kvb);
+    if (kv->held_in_mx) {
+      mx.c = kv->mx_layer(l);
+      launch_mx_attn(st, mx);
+      return;
+    }
+    at.k_cache = (char *)kv->k + (size_t)l * kv_layer;
+    at.v_cache = (char *)kv->v + (size_t)l * kv_layer;
     if (f32) launch_attn_f32(st, at); else launch_attn_bf16(st, at);
   };
 
@@ -631,7 +658,7 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
         g.k_norm_w = m->k_norm[l];
         launch_qkv_epilogue_f32(st, g, part);
       }
-      attention(kl, vl);
+      attention(l);
       g = base(EPI_RESID, attn_out, nullptr, qd, c.hidden);
       g.seg[0] = {m->wo[l], c.hidden, 0};
       g.x_resid = x; g.x_resid_out = x;
@@ -710,10 +737,19 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
       g.n_seg = 3;
       g.q_out = ws + L.q; g.q_panel = pan_q;
       g.cos_t = cos_t; g.sin_t = sin_t; g.qkv_f32 = qkv_f32; g.ctx = ctx;
-      g.k_cache = (char *)kv->k + (size_t)l * kv_layer;
-      g.v_cache = (char *)kv->v + (size_t)l * kv_layer;
       g.n_nodes = n_nodes; g.n_q_heads = c.n_q_heads; g.n_kv_heads = c.n_kv_heads; g.head_dim = c.head_dim;
-      g.kv = kv->map();
+      if (!kv->held_in_mx) {
+        g.k_cache = (char *)kv->k + (size_t)l * kv_layer;
+        g.v_cache = (char *)kv->v + (size_t)l * kv_layer;
+        g.kv = kv->map();
+      } else {
+        // the attention's launch quantises the fp32 rows; the epilogue's bf16 copies of the nodes alone go where the attention's result
+        // will be (4 rows kvd bytes of 4 rows_pad qd): the layer before has read its own, and nobody reads these
+        g.ctx = CtxLens{};
+        g.k_cache = attn_out;
+        g.v_cache = (bf16 *)attn_out + (size_t)rows * kvd;
+        g.kv = KvMap{nullptr, 0, 0, n_nodes, c.n_kv_heads, c.head_dim};
+      }
       g.q_norm_w = c.qk_norm ? m->q_norm[l] : nullptr;
       g.k_norm_w = c.qk_norm ? m->k_norm[l] : nullptr;
       return g;
@@ -816,9 +852,8 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
       o_tiles = ss_tiles_of(c.hidden, po.tile_n);
       dn_tiles = ss_tiles_of(c.hidden, pd.tile_n);
       for (int l = 0; l < c.n_layers; ++l) {
-        char *kl = (char *)kv->k + (size_t)l * kv_layer, *vl = (char *)kv->v + (size_t)l * kv_layer;
         timed_gemm(mk_qkv(l, pq, ss0_tiles), b_qkv);
-        attention(kl, vl);
+        attention(l);
         timed_gemm(mk_o(l, po, x, x, h), b_o);
         timed_gemm(mk_gu(l, pg, h), b_gu);
         timed_gemm(mk_dn(l, pd, x, x), b_dn);
@@ -828,8 +863,7 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
     } else {
       timed_gemm(mk_qkv(0, pq, 1), b_qkv);
       for (int l = 0; l < c.n_layers; ++l) {
-        char *kl = (char *)kv->k + (size_t)l * kv_layer, *vl = (char *)kv->v + (size_t)l * kv_layer;
-        attention(kl, vl);
+        attention(l);
         LayerArgs la;
         memset(&la, 0, sizeof(la));
         const bool more = l + 1 < c.n_layers;
@@ -1122,8 +1156,9 @@ int trispec_kv_commit(trispec_kv *kv, const int32_t *nodes_host, const int32_t *
   }
   if (any) {
     (void)hipGetLastError();
-    launch_kv_commit((hipStream_t)stream, c.dtype, kv->k, kv->v, c.n_layers, kv->layer_elems(), kv->batch, kv->map(),
-                     t);
+    if (kv->held_in_mx) launch_mx_commit((hipStream_t)stream, kv->mx, c.head_dim, kv->mx_slots, c.n_layers, kv->batch, t);
+    else launch_kv_commit((hipStream_t)stream, c.dtype, kv->k, kv->v, c.n_layers, kv->layer_elems(), kv->batch, kv->map(),
+                          t);
     if (hipGetLastError() != hipSuccess) return TRISPEC_ELAUNCH;
   }
   for (int b = 0; b < kv->batch; ++b) kv->ctx_len[b] += t.n[b];

@@ -3,6 +3,7 @@
 #include <vector>
 
 #include "internal.hpp"
+#include "mx.hpp"
 #include "plan.hpp"
 
 struct trispec_model {
@@ -25,6 +26,17 @@ struct trispec_kv {
   // paged cache: device page table [batch][max_pages] and the pool size; contiguous cache: nullptr, 0, 0
   const int32_t *page_table;
   int32_t max_pages, n_pages;
+  // held in 4 bits: layer 0 (k and v above are nullptr), and the slots of all blocks and kv heads of a layer
+  bool held_in_mx = false;
+  ts::MxMap mx = {};
+  size_t mx_slots = 0;
+  ts::MxMap mx_layer(int l) const {
+    ts::MxMap c = mx;
+    const size_t codes = mx_slots * l * (model->cfg.head_dim / 2), scales = mx_slots * l * (model->cfg.head_dim / ts::kMxBlock);
+    c.k_codes += codes; c.v_codes += codes;
+    c.k_scales += scales; c.v_scales += scales;
+    return c;
+  }
   // elements of one layer of K (= of V), and the slot map the kernels address the cache through
   size_t layer_elems() const {
     const trispec_model_config &c = model->cfg;

@@ -1,0 +1,145 @@
+// Rows into the 4-bit cache, rows out of it, and the move of a verified path inside it (layout: mx.hpp).
+#include "mx.hpp"
+
+namespace ts {
+
+template <int D, typename T>
+__global__ __launch_bounds__(256) void k_mx_append(MxAppendArgs a) {
+  const int h = blockIdx.y, b = blockIdx.z, first = a.start[b], n = a.count[b];
+  const int group = (first / kMxGroup + (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6)) * kMxGroup;
+  if (group >= first + n) return;
+  mx_store_group<D, T>(a.c, b, h, group, first, n, (const T *)a.k.p + (int64_t)b * a.k.seq + h * D, a.k.row,
+                       (const T *)a.v.p + (int64_t)b * a.v.seq + h * D, a.v.row);
+}
+
+template <int D, typename T>
+__global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
+  using L = MxLane<D>;
+  const int h = blockIdx.y, b = blockIdx.z, first = a.start[b], n = a.count[b];
+  const int group = (first / kMxGroup + (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6)) * kMxGroup;
+  if (group >= first + n) return;
+  const L l(threadIdx.x & 63);
+  const int i = group + l.s - first;
+  const size_t r = a.c.block(b, h, group);
+  const int at = a.c.in_block(group);
+  const bool live = i >= 0 && i < n;
+#pragma unroll
+  for (int p = 0; p < L::P; ++p) {
+    if (!live) continue;
+    if (a.k) {
+      const uint32_t w = *(const uint32_t *)(a.c.k_codes + MxOffsets<D>::k_codes(a.c, r, at + l.s) + l.feature(p) / 2);
+      const uint32_t s = a.c.k_scales[MxOffsets<D>::k_scales(a.c, r, at + l.s) + l.scale(p)];
+      store8((T *)a.k + (int64_t)b * a.k_seq + (int64_t)i * a.k_row + h * D + l.feature(p), mx_values(w, mx_scale(s, 0)));
+    }
+    if (a.v) {
+      const uint8_t *vc = a.c.v_codes + MxOffsets<D>::v_codes(a.c, r, at) + (l.feature(p) / 4) * 16 + 2 * l.s;
+      const uint32_t w = *(const uint16_t *)vc | (uint32_t) * (const uint16_t *)(vc + 16) << 16;
+      const uint32_t s = a.c.v_scales[MxOffsets<D>::v_scales(a.c, r, at) + 8 * l.scale(p) + l.s];
+      store8((T *)a.v + (int64_t)b * a.v_seq + (int64_t)i * a.v_row + h * D + l.feature(p), mx_values(w, mx_scale(s, 0)));
+    }
+  }
+}
+
+// workgroups of four groups of 8 slots over the longest sequence's range
+template <typename A>
+static int mx_groups(const A &a, int batch) {
+  int most = 0;
+  for (int b = 0; b < batch; ++b)
+    if (a.count[b] > 0) most = max(most, (a.start[b] + a.count[b] + kMxGroup - 1) / kMxGroup - a.start[b] / kMxGroup);
+  return (most + 3) / 4;
+}
+
+void launch_mx_append(hipStream_t st, const MxAppendArgs &a, int batch) {
+  const int n = mx_groups(a, batch);
+  if (n == 0) return;
+  const dim3 grid(n, a.c.n_kv, batch);
+  if (a.head_dim == 128) {
+    if (a.dtype == TRISPEC_F32) hipLaunchKernelGGL((k_mx_append<128, float>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_mx_append<128, bf16>), grid, dim3(256), 0, st, a);
+  } else {
+    if (a.dtype == TRISPEC_F32) hipLaunchKernelGGL((k_mx_append<64, float>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_mx_append<64, bf16>), grid, dim3(256), 0, st, a);
+  }
+}
+
+void launch_mx_read(hipStream_t st, const MxReadArgs &a, int batch) {
+  const int n = mx_groups(a, batch);
+  if (n == 0) return;
+  const dim3 grid(n, a.c.n_kv, batch);
+  if (a.head_dim == 128) {
+    if (a.dtype == TRISPEC_F32) hipLaunchKernelGGL((k_mx_read<128, float>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_mx_read<128, bf16>), grid, dim3(256), 0, st, a);
+  } else {
+    if (a.dtype == TRISPEC_F32) hipLaunchKernelGGL((k_mx_read<64, float>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_mx_read<64, bf16>), grid, dim3(256), 0, st, a);
+  }
+}
+
+// Commit of a verified path (k_kv_commit) in the 4-bit cache: codes and scales of the path's nodes move from slot
+// ctx + node[i] to slot ctx + i, read into registers whole before anything is written.
+template <int D>
+__global__ __launch_bounds__(256) void k_mx_commit(MxMap m, size_t slots_all, CommitTable t) {
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int n = t.n[b], ctx = t.ctx[b];
+  if (n == 0) return;   // uniform over the workgroup
+  const size_t layer = blockIdx.z * slots_all;
+  m.k_codes += layer * (D / 2); m.v_codes += layer * (D / 2);
+  m.k_scales += layer * (D / kMxBlock); m.v_scales += layer * (D / kMxBlock);
+  constexpr int KW = D / 8, VW = D / 4, SW = D / kMxBlock;   // words of a key, half words of a value, scales of either
+  constexpr int KN = kMaxNodes * KW / 256, VN = kMaxNodes * VW / 256, SN = kMaxNodes * SW / 256;
+  static_assert(SN >= 1, "every thread a scale");
+  auto word = [&](int slot, int w) {
+    return (uint32_t *)(m.k_codes + MxOffsets<D>::k_codes(m, m.block(b, h, slot), m.in_block(slot))) + w;
+  };
+  auto half = [&](int slot, int q) {
+    const int s = m.in_block(slot);
+    return (uint16_t *)(m.v_codes + MxOffsets<D>::v_codes(m, m.block(b, h, slot), s & ~7)) + q * 8 + (s & 7);
+  };
+  auto k_scale = [&](int slot, int w) { return m.k_scales + MxOffsets<D>::k_scales(m, m.block(b, h, slot), m.in_block(slot)) + w; };
+  auto v_scale = [&](int slot, int w) {
+    const int s = m.in_block(slot);
+    return m.v_scales + MxOffsets<D>::v_scales(m, m.block(b, h, slot), s & ~7) + 8 * w + (s & 7);
+  };
+  uint32_t kw[KN];
+  uint16_t vw[VN];
+  uint8_t ks[SN], vs[SN];
+#pragma unroll
+  for (int u = 0; u < KN; ++u) {
+    const int i = (tid + 256 * u) / KW, w = (tid + 256 * u) % KW;
+    if (i < n) kw[u] = *word(ctx + t.node[b][i], w);
+  }
+#pragma unroll
+  for (int u = 0; u < VN; ++u) {
+    const int i = (tid + 256 * u) / VW, w = (tid + 256 * u) % VW;
+    if (i < n) vw[u] = *half(ctx + t.node[b][i], w);
+  }
+#pragma unroll
+  for (int u = 0; u < SN; ++u) {
+    const int i = (tid + 256 * u) / SW, w = (tid + 256 * u) % SW;
+    if (i < n) { ks[u] = *k_scale(ctx + t.node[b][i], w); vs[u] = *v_scale(ctx + t.node[b][i], w); }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < KN; ++u) {
+    const int i = (tid + 256 * u) / KW, w = (tid + 256 * u) % KW;
+    if (i < n) *word(ctx + i, w) = kw[u];
+  }
+#pragma unroll
+  for (int u = 0; u < VN; ++u) {
+    const int i = (tid + 256 * u) / VW, w = (tid + 256 * u) % VW;
+    if (i < n) *half(ctx + i, w) = vw[u];
+  }
+#pragma unroll
+  for (int u = 0; u < SN; ++u) {
+    const int i = (tid + 256 * u) / SW, w = (tid + 256 * u) % SW;
+    if (i < n) { *k_scale(ctx + i, w) = ks[u]; *v_scale(ctx + i, w) = vs[u]; }
+  }
+}
+
+void launch_mx_commit(hipStream_t st, const MxMap &m, int head_dim, size_t slots_all, int n_layers, int batch, const CommitTable &t) {
+  const dim3 grid(m.n_kv, batch, n_layers);
+  if (head_dim == 128) hipLaunchKernelGGL(k_mx_commit<128>, grid, dim3(256), 0, st, m, slots_all, t);
+  else hipLaunchKernelGGL(k_mx_commit<64>, grid, dim3(256), 0, st, m, slots_all, t);
+}
+
+}  // namespace ts

@@ -335,6 +335,31 @@ inline AttnPlan plan_attn(int batch, int n_kv, int group, int head_dim, int n_no
   return best;
 }
 
+// ---- attention over the 4-bit cache (k_mx_attn): how query rows and keys are divided
+struct MxPlan {
+  int row_blocks, row_waves, n_row_groups, keys_per_split, n_splits, n_draft;
+};
+// group * n_nodes query rows per kv head over up to max_keys keys
+inline MxPlan plan_mx(int batch, int n_kv, int group, int n_nodes, bool own_nodes, long max_keys) {
+  const int p_rows = group * n_nodes;
+  MxPlan p;
+  p.row_blocks = p_rows <= 16 ? 1 : (p_rows <= 128 ? 2 : 4);
+  p.row_waves = p_rows <= 32 ? 1 : (p_rows <= 64 ? 2 : 4);
+  const int rows = 16 * p.row_blocks * p.row_waves, groups = 4 / p.row_waves;
+  p.n_row_groups = (p_rows + rows - 1) / rows;
+  p.n_draft = own_nodes ? (n_nodes + 31) / 32 : 0;
+  const int per_split = batch * n_kv * p.n_row_groups;
+  int want = (p.row_blocks == 1 ? 1024 : (p.row_blocks == 2 ? 512 : 256)) / per_split;
+  if (want > kMaxAttnSplits) want = kMaxAttnSplits;
+  if (want < 1) want = 1;
+  const int unit = 32 * groups;
+  long kps = ((max_keys + want - 1) / want + unit - 1) / unit * unit;
+  if (kps < 128) kps = 128;
+  p.n_splits = (int)((max_keys + kps - 1) / kps);
+  p.keys_per_split = (int)kps;
+  return p;
+}
+
 // ---- the plans of one model, made once: the matmuls of a pass depend on its rows only through the kind of panel
 
 // kinds of panels: 1 to 4 row blocks of 16, 6, 8, more than 128 rows

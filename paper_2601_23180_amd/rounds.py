@@ -13,7 +13,8 @@ from typing import Dict, List, Sequence
 import numpy as np
 import torch
 
-from .binding import (CRIT_MARGIN, MAX_NODES, RESAMPLE_RESIDUAL, TERNARY_SCRATCH_INTS, KVCache, Model, PagedKVCache, RoundInfo,
+from .binding import (CRIT_MARGIN, MAX_NODES, RESAMPLE_RESIDUAL, TERNARY_SCRATCH_INTS, KVCache, Model, MXKVCache, PagedKVCache,
+                      RoundInfo,
                       SampleRound, TernaryConfig, check, lib)
 
 
@@ -29,10 +30,11 @@ def _pass_dict(r) -> Dict[str, object]:
 
 class TernaryDecoder:
     def __init__(self, proxy: Model, target: Model, capacity: int, criterion: int = CRIT_MARGIN,
-                 max_nodes: int = MAX_NODES, paged: bool = False):
+                 max_nodes: int = MAX_NODES, paged: bool = False, mx: bool = False):
+        """paged: caches in pages behind a table; mx: caches held in 4 bits (bf16 models)."""
         self.proxy, self.target = proxy, target
-        cache = PagedKVCache if paged else KVCache
-        self.kv_p, self.kv_t = cache(proxy, 1, capacity), cache(target, 1, capacity)
+        self.kv_p, self.kv_t = (MXKVCache(m, 1, capacity, paged=paged) if mx else (PagedKVCache if paged else KVCache)(m, 1, capacity)
+                                for m in (proxy, target))
         self.criterion, self.max_nodes = criterion, max_nodes
         self.seq: List[int] = []
         self.target_passes = 0          # passes of the target that verified drafts (not catch-up)
