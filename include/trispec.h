@@ -285,9 +285,7 @@ int trispec_mx_read(const trispec_mx_cache *c, const trispec_mx_rows *k, const t
  */
 typedef struct {
   trispec_mx_rows q, k, v;
-  int32_t dtype, n_nodes, n_q_heads;
-  const int32_t *tree_parents;
-  int32_t append;
+  int32_t dtype, n_nodes, n_q_heads, append;
   void *out;
   int64_t out_row_stride;
   void *workspace;
@@ -296,7 +294,8 @@ typedef struct {
 } trispec_mx_attend_args;
 int trispec_mx_attend_workspace_bytes(int32_t batch, int32_t n_nodes, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                       size_t *bytes);
-int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, const trispec_mx_attend_args *a);
+int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, const int32_t *tree_parents,
+                      const trispec_mx_attend_args *a);
 
 /* A cache object over such memory, for bf16 models: every other call takes it like a bf16 one (trispec_verify, trispec_kv_commit,
  * trispec_ternary_*).  `c` describes layer 0; each array holds the model's n_layers layers one behind another.  A pass quantises the

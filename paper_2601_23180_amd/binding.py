@@ -8,8 +8,8 @@ the binding's entry points raises.
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import os
+import struct
 from typing import Callable, Dict, List, Optional, Sequence
 
 import numpy as np
@@ -116,9 +116,14 @@ class MXRows(C.Structure):
 
 class MXAttendArgs(C.Structure):
     _fields_ = [("q", MXRows), ("k", MXRows), ("v", MXRows), ("dtype", C.c_int32), ("n_nodes", C.c_int32),
-                ("n_q_heads", C.c_int32), ("tree_parents", C.POINTER(C.c_int32)), ("append", C.c_int32),
-                ("out", C.c_void_p), ("out_row_stride", C.c_int64), ("workspace", C.c_void_p),
-                ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
+                ("n_q_heads", C.c_int32), ("append", C.c_int32), ("out", C.c_void_p), ("out_row_stride", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
+
+
+# The operators of a layer take microseconds: their structures are packed into bytes (a twentieth of a Structure's time)
+_pack_rows = struct.Struct("Pqq").pack
+_pack_attend = struct.Struct("PqqPqqPqqiiiiPqPNP").pack
+assert struct.calcsize("Pqq") == C.sizeof(MXRows) and struct.calcsize("PqqPqqPqqiiiiPqPNP") == C.sizeof(MXAttendArgs)
 
 
 class TriSpecError(RuntimeError):
@@ -195,12 +200,12 @@ def lib() -> C.CDLL:
         l.trispec_timer_read.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_double),
                                          C.POINTER(C.c_double)]
         l.trispec_timer_destroy.argtypes = [C.c_void_p]
-        _pc, _pr = C.POINTER(MXCacheDesc), C.POINTER(MXRows)
+        _pc = C.POINTER(MXCacheDesc)
         l.trispec_mx_cache_bytes.argtypes = [_pc, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
-        l.trispec_mx_append.argtypes = [_pc, _pr, _pr, C.c_int32, _pi, _pi, C.c_void_p]
+        l.trispec_mx_append.argtypes = [_pc, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]   # structures or their bytes
         l.trispec_mx_read.argtypes = l.trispec_mx_append.argtypes
         l.trispec_mx_attend_workspace_bytes.argtypes = [C.c_int32] * 5 + [C.POINTER(C.c_size_t)]
-        l.trispec_mx_attend.argtypes = [_pc, _pi, C.POINTER(MXAttendArgs)]
+        l.trispec_mx_attend.argtypes = [_pc, C.c_void_p, C.c_void_p, C.c_void_p]
         l.trispec_kv_create_mx.argtypes = [C.c_void_p, _pc, C.POINTER(C.c_void_p)]
         _lib = l
     return _lib
@@ -458,6 +463,8 @@ class MXCache:
         check(lib().trispec_mx_cache_bytes(C.byref(self.desc), C.byref(a), C.byref(b)))
         assert a.value == k_codes.numel() == v_codes.numel() and b.value == k_scales.numel() == v_scales.numel()
         self.ref = C.byref(self.desc)
+        self.index = self.device.index
+        self._ints = struct.Struct(f"{self.batch}i").pack
         self._workspace_bytes: Dict[tuple, int] = {}
 
     @classmethod
@@ -471,16 +478,18 @@ class MXCache:
                    torch.zeros((blocks, n_kv_heads, slots // 8, head_dim // 4, 8, 2), **u8),
                    torch.zeros((blocks, n_kv_heads, slots // 8, head_dim // 32, 8), **u8), table)
 
-    def rows(self, t: torch.Tensor, n_heads: int, dtype: torch.dtype) -> MXRows:
-        if (t.dim() != 4 or t.shape[0] != self.batch or t.shape[2] != n_heads or t.shape[3] != self.head_dim or t.dtype != dtype
-                or t.device != self.device or t.stride(3) != 1 or (n_heads > 1 and t.stride(2) != self.head_dim)):
-            raise ValueError(f"a {dtype} tensor [{self.batch}, n, {n_heads}, {self.head_dim}] on {self.device} is wanted, the heads of a row side by side")
-        return MXRows(t.data_ptr(), t.stride(1), t.stride(0))
+    def rows(self, t: torch.Tensor, n: int, n_heads: int, dtype: torch.dtype):
+        """(address, row stride, sequence stride) of [batch, n, n_heads, d] rows."""
+        stride = t.stride()
+        if (t.shape != (self.batch, n, n_heads, self.head_dim) or t.dtype is not dtype or t.device != self.device or stride[3] != 1
+                or (stride[2] != self.head_dim and n_heads > 1)):
+            raise ValueError(f"a {dtype} tensor {(self.batch, n, n_heads, self.head_dim)} on {self.device} is wanted, the heads of a row side by side")
+        return t.data_ptr(), stride[1], stride[0]
 
-    def ints(self, v: Sequence[int]):
+    def ints(self, v: Sequence[int]) -> bytes:
         if len(v) != self.batch:
             raise ValueError(f"a number for each of the {self.batch} sequences is wanted")
-        return (C.c_int32 * self.batch)(*v)
+        return self._ints(*v)
 
     def workspace_bytes(self, n_nodes: int, n_q_heads: int) -> int:
         key = (n_nodes, n_q_heads)
@@ -500,71 +509,94 @@ def _mx_dtype(t: torch.dtype) -> int:
     return _MX_DTYPES[t]
 
 
-def _on_device(fn):
-    """Runs an operator with the cache's device current: allocations, the stream and the launch are its."""
-    @functools.wraps(fn)
-    def call(cache, *args, stream=None, **kw):
-        if stream is None and cache.device.index == torch.cuda.current_device():
-            return fn(cache, *args, stream=torch.cuda.current_stream().cuda_stream, **kw)
-        with torch.cuda.device(cache.device), torch.cuda.stream(stream):   # what is allocated here belongs to that stream
-            return fn(cache, *args, stream=torch.cuda.current_stream().cuda_stream, **kw)
-    return call
+def _elsewhere(cache: MXCache, stream) -> bool:
+    """Whether an operator is to run on another stream, or device, than the current one."""
+    if stream is None:
+        return cache.index != torch.cuda.current_device()
+    if stream.device != cache.device:
+        raise ValueError(f"a stream on {cache.device} is wanted")
+    return True
 
 
-@_on_device
+# the current stream of a device as a number, 30 times as fast as torch.cuda.current_stream().cuda_stream
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def mx_append(cache: MXCache, k: torch.Tensor, v: torch.Tensor, start: Sequence[int], count: Optional[Sequence[int]] = None,
               stream=None) -> None:
     """trispec_mx_append: rows i < count[b] (default: all) of k and v [batch, n, n_kv, d] into slots start[b] + i."""
-    kr, vr = cache.rows(k, cache.n_kv_heads, k.dtype), cache.rows(v, cache.n_kv_heads, k.dtype)
-    n = k.shape[1]
-    if v.shape[1] != n or (count is not None and max(count, default=0) > n):
+    if _elsewhere(cache, stream):
+        with torch.cuda.device(cache.device), torch.cuda.stream(stream):
+            return mx_append(cache, k, v, start, count)
+    if k.dim() != 4:
+        raise ValueError("mx_append: k [batch, n, n_kv, d] is wanted")
+    n, dtype = k.shape[1], k.dtype
+    rk, rv = cache.rows(k, n, cache.n_kv_heads, dtype), cache.rows(v, n, cache.n_kv_heads, dtype)
+    if count is None:
+        count = (n,) * cache.batch
+    elif max(count, default=0) > n:
         raise ValueError("mx_append: more rows are to be written than k and v hold")
-    check(lib().trispec_mx_append(cache.ref, C.byref(kr), C.byref(vr), _mx_dtype(k.dtype), cache.ints(start),
-                                  cache.ints([n] * cache.batch if count is None else count), stream))
+    if n == 0:
+        return
+    rc = lib().trispec_mx_append(cache.ref, _pack_rows(*rk), _pack_rows(*rv), _mx_dtype(dtype), cache.ints(start), cache.ints(count), _raw_stream(cache.index))
+    if rc:
+        check(rc)
 
 
-@_on_device
 def mx_read(cache: MXCache, start: Sequence[int], n: int, dtype: torch.dtype = torch.bfloat16, stream=None):
     """trispec_mx_read: (k, v) [batch, n, n_kv, d] of the slots start[b] .. start[b] + n."""
-    k, v = torch.empty((2, cache.batch, n, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=cache.device)
-    row = cache.n_kv_heads * cache.head_dim
+    if _elsewhere(cache, stream):
+        with torch.cuda.device(cache.device), torch.cuda.stream(stream):   # what is allocated here belongs to that stream
+            return mx_read(cache, start, n, dtype)
+    d = _mx_dtype(dtype)
+    k, v = torch.empty((2, cache.batch, n, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=cache.device).unbind(0)
     if n > 0:
-        kr, vr = MXRows(k.data_ptr(), row, n * row), MXRows(v.data_ptr(), row, n * row)
-        check(lib().trispec_mx_read(cache.ref, C.byref(kr), C.byref(vr), _mx_dtype(dtype), cache.ints(start), cache.ints([n] * cache.batch), stream))
+        row = cache.n_kv_heads * cache.head_dim
+        rc = lib().trispec_mx_read(cache.ref, _pack_rows(k.data_ptr(), row, n * row), _pack_rows(v.data_ptr(), row, n * row), d, cache.ints(start),
+                                   cache.ints((n,) * cache.batch), _raw_stream(cache.index))
+        if rc:
+            check(rc)
     return k, v
 
 
-@_on_device
 def mx_attend(cache: MXCache, ctx_len: Sequence[int], q: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
               parents: Optional[np.ndarray] = None, append: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """trispec_mx_attend: q [batch, n_nodes, n_q, d], k and v [batch, n_nodes, n_kv, d] (None: the cache alone), parents host int32
     [batch, n_nodes] (None: a chain).  Returns [batch, n_nodes, n_q, d] in q's dtype.  `workspace`: uint8, at least
     cache.workspace_bytes(n_nodes, n_q) long and 256-byte aligned; by default one is taken from torch's allocator."""
+    if _elsewhere(cache, stream):
+        with torch.cuda.device(cache.device), torch.cuda.stream(stream):
+            return mx_attend(cache, ctx_len, q, k, v, parents, append, workspace)
     if q.dim() != 4:
         raise ValueError("mx_attend: q [batch, n_nodes, n_q, d] is wanted")
-    b, m, heads, d = q.shape
-    a = MXAttendArgs()
-    a.q = cache.rows(q, heads, q.dtype)
-    if (k is None) != (v is None) or (k is not None and (k.shape[1] != m or v.shape[1] != m)):
+    shape, dtype, device = q.shape, q.dtype, cache.device
+    m, heads = shape[1], shape[2]
+    rq = cache.rows(q, m, heads, dtype)
+    if k is not None and v is not None:
+        rk, rv = cache.rows(k, m, cache.n_kv_heads, dtype), cache.rows(v, m, cache.n_kv_heads, dtype)
+    elif k is None and v is None:
+        rk = rv = (0, 0, 0)
+    else:
         raise ValueError("mx_attend: keys and values of all nodes, or of none, are wanted")
-    if k is not None:
-        a.k, a.v = cache.rows(k, cache.n_kv_heads, q.dtype), cache.rows(v, cache.n_kv_heads, q.dtype)
     if parents is not None:
-        parents = np.ascontiguousarray(parents, dtype=np.int32)
-        if parents.shape != (b, m):
+        parents = np.asarray(parents)
+        if parents.shape != shape[:2]:
             raise ValueError("mx_attend: a parent for each node is wanted")
-        a.tree_parents = parents.ctypes.data_as(C.POINTER(C.c_int32))
-    a.dtype, a.n_nodes, a.n_q_heads, a.append = _mx_dtype(q.dtype), m, heads, int(append)
+        parents = (parents if parents.dtype == np.int32 else parents.astype(np.int32)).tobytes()
     need = cache.workspace_bytes(m, heads)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
-    elif workspace.device != cache.device or not workspace.is_contiguous():
+        workspace, have = torch.empty(need, dtype=torch.uint8, device=device), need
+    elif workspace.device != device or not workspace.is_contiguous():
         raise ValueError("mx_attend: a contiguous workspace on the cache's device is wanted")
-    out = torch.empty((b, m, heads, d), dtype=q.dtype, device=cache.device)
-    a.out, a.out_row_stride = out.data_ptr(), heads * d
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    a.stream = stream
-    check(lib().trispec_mx_attend(cache.ref, cache.ints(ctx_len), C.byref(a)))
+    else:
+        have = workspace.numel() * workspace.element_size()
+    out = torch.empty(shape, dtype=dtype, device=device)
+    rc = lib().trispec_mx_attend(cache.ref, cache.ints(ctx_len), parents, _pack_attend(
+        *rq, *rk, *rv, _mx_dtype(dtype), m, heads, 1 if append else 0, out.data_ptr(), heads * cache.head_dim, workspace.data_ptr(), have,
+        _raw_stream(cache.index)))
+    if rc:
+        check(rc)
     return out
 
 

@@ -556,8 +556,8 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
     mx.batch = B; mx.n_nodes = n_nodes; mx.n_q_heads = c.n_q_heads; mx.group = group; mx.head_dim = c.head_dim;
     mx.dtype = TRISPEC_F32;
     mx.append = 1;
-    mx.row_blocks = p.row_blocks; mx.row_waves = p.row_waves; mx.n_row_groups = p.n_row_groups;
-    mx.keys_per_split = p.keys_per_split; mx.n_splits = p.n_splits; mx.n_draft = p.n_draft;
+    mx.form = p.form; mx.n_row_groups = p.n_row_groups;
+    mx.n_splits = p.n_splits; mx.n_own = p.n_own;
     mx.part_o = (float *)(ws + L.attn_o);
     mx.part_m = (float *)(ws + L.attn_m);
     mx.part_l = (float *)(ws + L.attn_l);

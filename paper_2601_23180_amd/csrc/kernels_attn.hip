@@ -10,7 +10,9 @@
 // copies for later rounds, but the pass itself never reads them back.  Where they are evaluated is up to
 // the host (AttnArgs::draft_mode): in blocks of 32 by workgroups of the same launch, or by the merge
 // kernel, which combines all partials of a row in ascending order.
-#include "attn_draft.hpp"
+#include <float.h>
+
+#include "device_util.hpp"
 
 namespace ts {
 
@@ -137,16 +139,122 @@ __device__ __forceinline__ void split_pair(f32x2 p, bf16x8 &hi, bf16x8 &lo, int 
   lo[e] = l[0]; lo[e + 1] = l[1];
 }
 
-// draft_partial of block kb for (sequence, kv head), into partial `part_base`
+// Maximum, in natural-log units, that a partial is stored with.  -inf marks a partial without keys, which the
+// merge skips without reading it; one whose scores are all NaN (fmaxf drops them) or all -inf has to be
+// added up all the same, so that the NaN in its sums reaches the row: it is stored with the lowest finite value.
+__device__ __forceinline__ float stored_max(float m_log2) { return fmaxf(m_log2 * 0.693147180559945f, -FLT_MAX); }
+
+// Softmax partial of 32 query rows (one wavefront) over the draft nodes 32 kb .. 32 kb + 31: S^T = K Q^T
+// and O^T = V^T P^T with fp32 matrix instructions (32x32x2), operands straight from the projections.
+// Lane (ln, g) holds features g D/2 .. of key / query row ln for the first product; the scores come out
+// with keys 8q + 4g + r in register 4q + r, which is the order in which the second product takes them.
+// 128 instructions of 64 cycles, 3.5 us, beside context workgroups that run longer.  Evaluated by the
+// merge kernel, where every row fetches its ancestors' keys and values for itself, a chain of 128 nodes
+// with 32 heads takes 44 us a layer; the plain merge takes 8.4, the launch before it 18.6 instead of 16.1.
+// s_p: 32 x 32 floats of LDS of this wavefront.
 template <int D>
-__device__ __forceinline__ void draft_block(const AttnArgs &a, int kb, int kvh, int b, int row_block, size_t part_base, float *s_p) {
-  const int M = a.n_nodes, group = a.n_q_heads / a.n_kv_heads;
-  const int64_t n_total = (int64_t)(a.n_q_heads + 2 * a.n_kv_heads) * D;
+__device__ void draft_partial(const AttnArgs &a, int kb, int kvh, int b, int row_block, size_t part_base, float *s_p) {
+  const int lane = threadIdx.x & 63, ln = lane & 31, g = lane >> 5;
+  const int M = a.n_nodes, group = a.n_q_heads / a.n_kv_heads, p_rows = group * M;
+  const int prow = row_block * 32 + ln;
+  if (row_block * 32 >= p_rows) return;   // wave-uniform
+  const int pc = min(prow, p_rows - 1), al = pc / M, node = pc - al * M;
+  const AncMask mask = a.anc[b * M + node];
+  const uint32_t mine = (uint32_t)((kb < 2 ? mask.lo : mask.hi) >> (32 * (kb & 1)));   // ancestors in this block
+  const size_t pi = part_base * p_rows + prow;
+  if (__builtin_amdgcn_ballot_w64(mine != 0) == 0) {   // none for any row
+    if (prow < p_rows && g == 0) { a.part_m[pi] = -INFINITY; a.part_l[pi] = 0.f; }
+    return;
+  }
+  const size_t n_total = (size_t)(a.n_q_heads + 2 * a.n_kv_heads) * D;
   const float *base = a.qkv + (size_t)b * M * n_total;
-  const DraftRows<float> src = {base + kvh * group * D, base + (a.n_q_heads + kvh) * D, base + (a.n_q_heads + a.n_kv_heads + kvh) * D,
-                                n_total, n_total, n_total};
-  const size_t row = part_base * (group * M);
-  draft_partial<D>(src, [&](int node) { return a.anc[b * M + node]; }, M, group, kb, row_block, a.part_m + row, a.part_l + row, a.part_o + row * D, s_p);
+  const float *kp = base + min(kb * 32 + ln, M - 1) * n_total + (size_t)(a.n_q_heads + kvh) * D + g * (D / 2);
+  const float *qp = base + node * n_total + (size_t)(kvh * group + al) * D + g * (D / 2);
+  f32x16 s0, s1;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s0[e] = s1[e] = 0.f;
+  {
+    f32x4 kv[D / 8], qv[D / 8];
+#pragma unroll
+    for (int t = 0; t < D / 8; ++t) { kv[t] = *(const f32x4 *)(kp + 4 * t); qv[t] = *(const f32x4 *)(qp + 4 * t); }
+#pragma unroll
+    for (int t = 0; t < D / 8; ++t) {
+      s0 = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[t][0], qv[t][0], s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[t][1], qv[t][1], s1, 0, 0, 0);
+      s0 = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[t][2], qv[t][2], s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[t][3], qv[t][3], s1, 0, 0, 0);
+    }
+  }
+  const float *vp = base + (size_t)(a.n_q_heads + a.n_kv_heads + kvh) * D;
+  float v[16][D / 32];   // all values in one round trip, behind the softmax
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+      v[e][db] = vp[min(kb * 32 + 8 * (e >> 2) + 4 * g + (e & 3), M - 1) * n_total + db * 32 + ln];
+  __builtin_amdgcn_sched_barrier(0);
+  const float scale = 1.44269504088896f / sqrtf((float)D);
+  float p[16], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int key = 8 * (e >> 2) + 4 * g + (e & 3);
+    p[e] = (mine >> key) & 1u ? (s0[e] + s1[e]) * scale : -INFINITY;
+    m = fmaxf(m, p[e]);
+  }
+  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  const float m_safe = m == -INFINITY ? 0.f : m;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    p[e] = __builtin_amdgcn_exp2f(p[e] - m_safe);   // 0 for other branches
+    l += p[e];
+  }
+  l += __shfl_xor(l, 32, 64);
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
+  float finite = 0.f;   // stays 0 while every value is finite
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      finite = __builtin_fmaf(v[e][db], 0.f, finite);
+      o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e][db], p[e], o[db], 0, 0, 0);
+    }
+  if (__builtin_amdgcn_ballot_w64(finite != 0.f) != 0) {
+    // an infinity or NaN among the values: a weight of 0 would carry it into rows of other branches.
+    // Row by row over the ancestors only.
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s_p[(8 * (e >> 2) + 4 * g + (e & 3)) * 32 + ln] = p[e];
+    __builtin_amdgcn_s_waitcnt(0);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < 32; ++k) {
+      if (!((mine >> k) & 1u)) continue;
+      const float w = s_p[k * 32 + ln];
+      const float *vr = vp + (kb * 32 + k) * n_total + 4 * g;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[db][e] += w * vr[db * 32 + 8 * (e >> 2) + (e & 3)];
+    }
+  }
+  if (prow >= p_rows) return;
+  if (g == 0) {
+    a.part_m[pi] = mine != 0 ? stored_max(m) : -INFINITY;
+    a.part_l[pi] = l;
+  }
+  float *out = a.part_o + pi * D;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *(f32x4 *)(out + db * 32 + 8 * q + 4 * g) = f32x4{o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]};
 }
 
 // NW wavefronts; KG groups of them take KT / KG keys of every tile each, the NW / KG wavefronts of a group a
@@ -179,7 +287,7 @@ __global__ __launch_bounds__(64 * NW) void k_attn_bf16(AttnArgs a) {
   const size_t part_base = ((size_t)b * a.n_kv_heads + kvh) * (a.n_splits + a.n_draft) + split;
   if constexpr (DRAFT) {
     if (split >= a.n_splits) {
-      if (kg == 0) draft_block<D>(a, split - a.n_splits, kvh, b, rg * RB + rb, part_base, (float *)lds + wave * 1024);
+      if (kg == 0) draft_partial<D>(a, split - a.n_splits, kvh, b, rg * RB + rb, part_base, (float *)lds + wave * 1024);
       return;
     }
   }
@@ -500,7 +608,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_few(AttnArgs a) {
   const int M = a.n_nodes, group = a.n_q_heads / a.n_kv_heads, p_rows = group * M;
   const size_t part_base = ((size_t)b * a.n_kv_heads + kvh) * (a.n_splits + a.n_draft) + split;
   if (split >= a.n_splits) {
-    if (wave < RB) draft_block<D>(a, split - a.n_splits, kvh, b, wave, part_base, s_o + wave * 1024);
+    if (wave < RB) draft_partial<D>(a, split - a.n_splits, kvh, b, wave, part_base, s_o + wave * 1024);
     return;
   }
   const int ctx = a.ctx.v[b], k_begin = split * a.keys_per_split, k_end = min(ctx, k_begin + a.keys_per_split);
@@ -658,6 +766,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_few(AttnArgs a) {
 // last partial would fetch it again, and its registers cost wavefronts in flight: 128 nodes, 12 partials, 8.0 us
 // with 20 requested, 6.8 with 12).  Block = group * d / 2 threads, two adjacent output features each.
 constexpr int kMergeBatch = 20;   // 16 context splits and the draft blocks of 128 nodes
+// e^x through the hardware exp2 (about 1e-7 |x| relative error; the arguments here are <= 0)
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
 
 template <int D, int NB>
 __global__ __launch_bounds__(512) void k_attn_merge(AttnArgs a) {

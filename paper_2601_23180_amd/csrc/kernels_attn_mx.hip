@@ -10,440 +10,654 @@
 // reduction is chosen so that nothing moves between lanes: score register e of lane (ln, g) is the key 8 g + e of the
 // tile, which is what the second product's operand wants of that lane.  bf16 queries are exact operands and probabilities
 // are rounded to bf16, half a step of the result's own type; fp32 ones go as high part + low part, both.
-#include "attn_draft.hpp"
+#include <float.h>
+
 #include "mx.hpp"
+#include "plan.hpp"
 
 namespace ts {
 
 namespace {
 
-template <typename T>
-struct Parts {   // of an operand
-  static constexpr int N = 1;
-};
-template <>
-struct Parts<float> {
-  static constexpr int N = 2;
-};
+// Maximum, in natural-log units, that a partial is stored with, as kernels_attn.hip has it: -inf marks a partial without keys, which the
+// merge skips; one whose scores are all NaN or all -inf is added up, so that the NaN in its sums reaches the row.
+__device__ __forceinline__ float stored_max(float m_log2) { return fmaxf(m_log2 * 0.693147180559945f, -FLT_MAX); }
 
-// Eight queries as operands: part 0 high, part 1 the rest
-__device__ __forceinline__ void query_parts(const bf16 *p, bf16x8 (&q)[1]) { q[0] = *(const bf16x8 *)p; }
-__device__ __forceinline__ void query_parts(const float *p, bf16x8 (&q)[2]) {
-#pragma unroll
-  for (int e = 0; e < 8; e += 4) {
-    const f32x4 x = *(const f32x4 *)(p + e);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      q[0][e + i] = (bf16)x[i];
-      q[1][e + i] = (bf16)(x[i] - (float)q[0][e + i]);
-    }
+// A number as NP bf16 parts, each the largest that fits of what is left.  bf16 inputs are one part; fp32 ones three, which is all 24 bits, or
+// two (rounded: 16 bits) in a verification pass, whose activations go to every product that way.
+template <int NP>
+__device__ __forceinline__ void split_value(float x, bf16 (&o)[NP]) {
+  if constexpr (NP == 1) {
+    o[0] = (bf16)x;
+  } else if constexpr (NP == 2) {
+    o[0] = (bf16)x;
+    o[1] = (bf16)(x - (float)o[0]);
+  } else {   // cut off, not rounded: exact, and nothing finite becomes infinite
+    const float a = __uint_as_float(__float_as_uint(x) & 0xffff0000u), y = x - a;
+    const float b = __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+    o[0] = (bf16)a; o[1] = (bf16)b; o[2] = (bf16)(y - b);
   }
 }
-__device__ __forceinline__ void prob_parts(f32x2 p, bf16x8 (&o)[1], int e) {
-  const bf16x2 h = __builtin_convertvector(p, bf16x2);
-  o[0][e] = h[0]; o[0][e + 1] = h[1];
+// Eight queries, keys or values as operands
+template <int NP>
+__device__ __forceinline__ void split8(const f32x4 &x, const f32x4 &y, bf16x8 (&o)[NP]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    bf16 parts[NP];
+    split_value<NP>(e < 4 ? x[e & 3] : y[e & 3], parts);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) o[p][e] = parts[p];
+  }
 }
-__device__ __forceinline__ void prob_parts(f32x2 p, bf16x8 (&o)[2], int e) {
-  const bf16x2 h = __builtin_convertvector(p, bf16x2);
-  const f32x2 rest = {p[0] - (float)h[0], p[1] - (float)h[1]};
-  const bf16x2 l = __builtin_convertvector(rest, bf16x2);
-  o[0][e] = h[0]; o[0][e + 1] = h[1];
-  o[1][e] = l[0]; o[1][e + 1] = l[1];
+template <int NP>
+__device__ __forceinline__ void load_parts(const float *p, bf16x8 (&o)[NP]) { split8<NP>(*(const f32x4 *)p, *(const f32x4 *)(p + 4), o); }
+template <int NP>
+__device__ __forceinline__ void load_parts(const bf16 *p, bf16x8 (&o)[NP]) {
+  static_assert(NP == 1, "bf16 operands are exact");
+  o[0] = *(const bf16x8 *)p;
+}
+// Two probabilities, elements e and e + 1
+template <int NP>
+__device__ __forceinline__ void prob_parts(f32x2 p, bf16x8 (&o)[NP], int e) {
+  f32x2 rest = p;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const bf16x2 h = __builtin_convertvector(rest, bf16x2);
+    o[i][e] = h[0]; o[i][e + 1] = h[1];
+    if (i + 1 < NP) rest = f32x2{rest[0] - (float)h[0], rest[1] - (float)h[1]};
+  }
 }
 
-// A wavefront's 32 keys as they lie in the cache.  Lane (ln, g): of key 8 (ln / 4) + 4 t + ln % 4, t = 0, 1, the features
-// (D / 4) g .., inside one block; of the keys 8 g .. 8 g + 7 the values of features 64 i + 4 ln .. + 3.
+// A wavefront's 32 keys as they lie in the cache, from slot s of block row r.  Lane (ln, g): of key 8 (ln / 4) + 4 t + ln % 4, t = 0, 1,
+// the features (D / 4) g .., inside one block; of the keys 8 g .. 8 g + 7 the values of features 64 i + 4 ln .. + 3.
 template <int D>
 struct KeyCodes {
   uint32_t w[2][D / 32];
   uint32_t scale[2];
+  __device__ __forceinline__ void load(const MxMap &m, size_t r, int s, uint32_t ln, uint32_t g) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) load(m, r, s, ln, g, t, t);
+  }
+  // run t's into place `to`.  Uniform bases and 32-bit lane offsets: the address arithmetic stays off the vector ALU
+  __device__ __forceinline__ void load(const MxMap &m, size_t r, int s, uint32_t ln, uint32_t g, int t, int to) {
+    const uint8_t *codes = m.k_codes + MxOffsets<D>::k_codes(m, r, s + 4 * t), *scales = m.k_scales + MxOffsets<D>::k_scales(m, r, s + 4 * t);
+    const uint32_t at = 8 * (ln >> 2) + (ln & 3);
+    if constexpr (D == 128) {
+      const u32x4 x = *(const u32x4 *)(codes + (at * (D / 2) + g * (D / 8)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[to][i] = x[i];
+    } else {
+      const u32x2 x = *(const u32x2 *)(codes + (at * (D / 2) + g * (D / 8)));
+      w[to][0] = x[0]; w[to][1] = x[1];
+    }
+    scale[to] = scales[at * (D / 32) + g * (D / 32) / 4];
+  }
+  // operand of reduction step i for 16 keys: features (D / 4) g + 8 i ..
+  __device__ __forceinline__ bf16x8 operand(int t, int i) const { return mx_values(w[t][i], mx_scale(scale[t], 0)); }
 };
 template <int D>
 struct ValueCodes {
   u32x4 w[D / 64];
   u32x2 scale[D / 64];
+  __device__ __forceinline__ void load(const MxMap &m, size_t r, int s, uint32_t ln, uint32_t g) {
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) load(m, r, s, ln, g, i, i);
+  }
+  // the 64 features from 64 i on into place `to`
+  __device__ __forceinline__ void load(const MxMap &m, size_t r, int s, uint32_t ln, uint32_t g, int i, int to) {
+    w[to] = *(const u32x4 *)(m.v_codes + MxOffsets<D>::v_codes(m, r, s) + 256 * i + (g * (8 * D / 2) + ln * 16));
+    scale[to] = *(const u32x2 *)(m.v_scales + MxOffsets<D>::v_scales(m, r, s) + 16 * i + (g * (8 * D / 32) + (ln >> 3) * 8));
+  }
+  // only the first `left` of the lane's eight keys are tokens: the others become element 0 of the smallest scale, whatever lies there
+  __device__ __forceinline__ void keep(int left) {
+    const uint64_t mask = left <= 0 ? 0 : (left >= 8 ? ~0ull : (1ull << (8 * left)) - 1);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      scale[i][0] &= (uint32_t)mask;
+      scale[i][1] &= (uint32_t)(mask >> 32);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[i][x] &= (2 * x < left ? 0xffffu : 0u) | (2 * x + 1 < left ? 0xffff0000u : 0u);
+    }
+  }
+  // operands of the features 64 i + 4 ln + j, j = 0 .. 3: the eight keys of the lane
+  __device__ __forceinline__ void operands(int i, bf16x8 (&o)[4]) const {
+    uint32_t f[4][4];   // [feature][pair of keys]
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float s0 = mx_scale(scale[i][x >> 1], (2 * x) & 3), s1 = mx_scale(scale[i][x >> 1], (2 * x + 1) & 3);
+      union { bf16x2 v; uint32_t u; } a0, a1, b0, b1;   // features 0, 1 and 2, 3 of both keys
+      a0.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i][x], s0, 0); a1.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i][x], s1, 2);
+      b0.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i][x], s0, 1); b1.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i][x], s1, 3);
+      f[0][x] = __builtin_amdgcn_perm(a1.u, a0.u, 0x05040100); f[1][x] = __builtin_amdgcn_perm(a1.u, a0.u, 0x07060302);
+      f[2][x] = __builtin_amdgcn_perm(b1.u, b0.u, 0x05040100); f[3][x] = __builtin_amdgcn_perm(b1.u, b0.u, 0x07060302);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = __builtin_bit_cast(bf16x8, u32x4{f[j][0], f[j][1], f[j][2], f[j][3]});
+  }
 };
+
+// RB blocks of 16 query rows of a wavefront: their queries as operands, and the running sums.
+//
+// Probabilities are powers of two relative to a reference r per row, which is set kHead above the largest score of the row when one
+// outgrows it: they stay at 1 and below, nothing finite overflows, and the reference, and with it the sums, moves once or twice on a long
+// context instead of with every new maximum (32 rows have one in 60 % of 64 runs of random keys).  Whether a score has outgrown r is seen
+// from the probabilities.  The sum of a row's weights comes from the matrix cores as one more feature that is 1.
+constexpr float kHead = 8.f;
+template <int D, int RB, typename T, int NP>
+struct QueryRows {
+  static constexpr int ST = D / 32, NV = D / 64, NO = 4 * NV;
+  bf16x8 q[RB][ST][NP];   // lane (ln, g): features (D / 4) g + 8 t .. of row ln of each block
+  float r[RB];
+  f32x4 o[RB][NO + 1];    // o[rb][4 i + j][e]: feature 64 i + 16 g + 4 e + j of row ln; o[rb][NO]: the sum of its weights, four times
+
+  static __device__ __forceinline__ float unit() { return 1.44269504088896f / sqrtf((float)D); }   // scores in powers of two
+  __device__ __forceinline__ void start(const MxAttnArgs &a, const T *q0, int first_row, int p_rows, int ln, int g) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int pc = min(first_row + rb * 16 + ln, p_rows - 1), al = pc / a.n_nodes, node = pc - al * a.n_nodes;
+      const T *p = q0 + node * a.q.row + al * D + g * (D / 4);
+#pragma unroll
+      for (int t = 0; t < ST; ++t) load_parts<NP>(p + 8 * t, q[rb][t]);
+      r[rb] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i <= NO; ++i) o[rb][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  static __device__ __forceinline__ void clear(f32x4 (&s)[RB][2]) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) s[rb][0] = s[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // scores += step i of the reduction; kf: 2 x 16 keys
+  __device__ __forceinline__ void score(f32x4 (&s)[RB][2], const bf16x8 &kf0, const bf16x8 &kf1, int i) const {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        s[rb][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf0, q[rb][i][p], s[rb][0], 0, 0, 0);
+        s[rb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf1, q[rb][i][p], s[rb][1], 0, 0, 0);
+      }
+  }
+  // leaves the lane's keys out whose bits are not set
+  static __device__ __forceinline__ void mask(f32x4 (&s)[2], uint32_t bits) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!((bits >> e) & 1u)) s[e >> 2][e & 3] = -INFINITY;
+  }
+  // returns the largest
+  static __device__ __forceinline__ float powers(const f32x4 (&s)[2], float ref, bf16x8 (&pf)[NP]) {
+    float p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][e & 3], unit(), -ref));   // 0 for a key left out
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) prob_parts<NP>(f32x2{p[e], p[e + 1]}, pf, e);
+    return fmaxf(fmaxf(fmaxf(fmaxf(p[0], p[1]), p[2]), fmaxf(fmaxf(p[3], p[4]), p[5])), fmaxf(p[6], p[7]));
+  }
+  // scores to probabilities, as operands; the largest, or a number above 1 where a lane has none (keys left out before the first one, NaN scores)
+  __device__ __forceinline__ float weigh(const f32x4 (&s)[RB][2], bf16x8 (&pf)[RB][NP]) const {
+    float top = 0.f;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const float t = powers(s[rb], r[rb], pf[rb]);
+      top = t <= 1.f ? fmaxf(top, t) : 2.f;
+    }
+    return top;
+  }
+  // behind weigh: where a score has outgrown its row's reference, the reference and the sums move and the probabilities are taken again
+  __device__ __forceinline__ void settle(const f32x4 (&s)[RB][2], bf16x8 (&pf)[RB][NP], float top) {
+    if (__builtin_amdgcn_ballot_w64(top > 1.f) == 0) return;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float t = fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3]));
+      t = fmaxf(t, fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3])));
+      t = fmaxf(t, __shfl_xor(t, 16, 64));
+      t = fmaxf(t, __shfl_xor(t, 32, 64)) * unit();
+      const float r_new = t > r[rb] ? t + kHead : r[rb], alpha = t > r[rb] ? __builtin_amdgcn_exp2f(r[rb] - r_new) : 1.f;   // 0 at first
+      r[rb] = r_new;
+#pragma unroll
+      for (int i = 0; i <= NO; ++i) o[rb][i] *= alpha;
+      powers(s[rb], r_new == -INFINITY ? 0.f : r_new, pf[rb]);
+    }
+  }
+  // sums += values of 16 features (i < NO; NO: the ones) times probabilities
+  __device__ __forceinline__ void add(const bf16x8 &vf, const bf16x8 (&pf)[RB][NP], int i) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) o[rb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb][p], o[rb][i], 0, 0, 0);
+  }
+  static __device__ __forceinline__ bf16x8 ones() {
+    const bf16 x = (bf16)1.f;
+    return bf16x8{x, x, x, x, x, x, x, x};
+  }
+  // What infinities and NaNs among the values of the nodes 32 kb .. add to the rows that see them (sees).  They are left out of the products,
+  // where a weight of 0 would carry them into rows of other branches.
+  __device__ __forceinline__ void add_odd(const T *v, int64_t v_row, int kb, const uint32_t (&sees)[RB], const bf16x8 (&pf)[RB][NP]) {
+    const int lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
+#pragma unroll 1
+    for (int n = 0; n < 32; ++n)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float w = 0.f;   // of node n, in the lane that holds it
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w = (n & 7) == e ? (float)pf[rb][0][e] : w;
+        w = __shfl(w, ln + 16 * (n >> 3), 64);
+        if (!((sees[rb] >> n) & 1u)) continue;   // an ancestor is a node of the tree
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const f32x4 y = load4(v + (32 * kb + n) * v_row + 64 * i + 16 * g + 4 * e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (!(__builtin_fabsf(y[j]) < INFINITY)) o[rb][4 * i + j][e] += w * y[j];
+          }
+      }
+  }
+};
+
+// The draft nodes of one (sequence, kv head)
+template <typename T>
+struct OwnRows {
+  const T *k, *v;
+  int64_t k_row, v_row;
+  int M;
+  __device__ __forceinline__ OwnRows(const MxAttnArgs &a, int kvh, int b, int d)
+      : k((const T *)a.k.p + b * a.k.seq + kvh * d), v((const T *)a.v.p + b * a.v.seq + kvh * d), k_row(a.k.row), v_row(a.v.row), M(a.n_nodes) {}
+};
+
+// Root paths of sequence b.  A tree given by its parents is turned into them in LDS (lds: kPathBytes): every node takes over what lies above it,
+// twice as far each time.  Every thread of the workgroup comes here.
+constexpr int kPathBytes = kMaxNodes * 20;
+struct RootPaths {
+  const MxAttnArgs &a;
+  const uint64_t *lo, *hi;
+  int b;
+  __device__ __forceinline__ RootPaths(const MxAttnArgs &args, unsigned char *lds, int seq) : a(args), lo((uint64_t *)lds), hi(lo + kMaxNodes), b(seq) {
+    if (a.anc || a.chain) return;
+    uint64_t *l = (uint64_t *)lds, *h = l + kMaxNodes;
+    int32_t *up = (int32_t *)(h + kMaxNodes);
+    const int i = threadIdx.x, M = a.n_nodes;
+    if (i < M) {
+      AncMask m = {0, 0};
+      m.set(i);
+      l[i] = m.lo; h[i] = m.hi;
+      up[i] = a.parent[b * M + i];
+    }
+    __syncthreads();
+    for (int far = 1; far < M; far *= 2) {
+      uint64_t x = 0, y = 0;
+      int32_t u = 0;
+      if (i < M) { u = up[i]; x = l[i] | l[u]; y = h[i] | h[u]; u = up[u]; }
+      __syncthreads();
+      if (i < M) { l[i] = x; h[i] = y; up[i] = u; }
+      __syncthreads();
+    }
+  }
+  __device__ __forceinline__ AncMask of(int node) const {
+    if (a.anc) return a.anc[b * a.n_nodes + node];
+    if (a.chain) return AncMask{node < 63 ? (2ull << node) - 1 : ~0ull, node < 64 ? 0ull : (node < 127 ? (2ull << (node - 64)) - 1 : ~0ull)};
+    return AncMask{lo[node], hi[node]};
+  }
+};
+
+// Softmax sums of 16 query rows over draft nodes n_begin .. n_end, by one wavefront with 16 x 16 x 4 fp32 instructions, 16 nodes at a time.
+// Lane (ln, g): features D/4 g .. of node / query row ln for the scores, which come out as nodes 4 g + e of row ln; features D/16 ln .. of the
+// nodes 4 g + e for the second product.
+template <int D, typename T>
+struct OwnSums {
+  static constexpr int F = D / 16;   // features a lane takes
+  float m, l;       // of row ln; m in powers of two
+  f32x4 o[F];       // o[f][e]: feature (4 g + e) F + f
+  __device__ __forceinline__ void store(float *row) const {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int f = 0; f < F; f += 4) *(f32x4 *)(row + (4 * g + e) * F + f) = f32x4{o[f][e], o[f + 1][e], o[f + 2][e], o[f + 3][e]};
+  }
+  __device__ __forceinline__ OwnSums(const OwnRows<T> &x, const T *q, const AncMask &path, int n_begin, int n_end) {
+    const int lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
+    const float scale = 1.44269504088896f / sqrtf((float)D);
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int f = 0; f < F; ++f) o[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int n0 = n_begin; n0 < n_end; n0 += 16) {
+      const uint32_t mine = (uint32_t)((n0 < 64 ? path.lo : path.hi) >> (n0 & 63)) & 0xffffu;
+      if (__builtin_amdgcn_ballot_w64(mine != 0) == 0) continue;
+      const T *kp = x.k + min(n0 + ln, x.M - 1) * x.k_row + g * (D / 4), *qp = q + g * (D / 4);
+      f32x4 s0 = f32x4{0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+      for (int t = 0; t < D / 16; t += 4) {
+        f32x4 kv[4], qv[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (t + u < D / 16) { kv[u] = load4(kp + 4 * (t + u)); qv[u] = load4(qp + 4 * (t + u)); }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (t + u < D / 16) {
+            s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[u][0], qv[u][0], s0, 0, 0, 0);
+            s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[u][1], qv[u][1], s1, 0, 0, 0);
+            s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[u][2], qv[u][2], s0, 0, 0, 0);
+            s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[u][3], qv[u][3], s1, 0, 0, 0);
+          }
+      }
+      float p[4], top = m;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = (mine >> (4 * g + e)) & 1u ? (s0[e] + s1[e]) * scale : -INFINITY;
+        top = fmaxf(top, p[e]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float m_safe = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - m_safe);
+      m = top;
+      l *= alpha;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(p[e] - m_safe);   // 0 for other branches
+        l += p[e];
+      }
+#pragma unroll
+      for (int f0 = 0; f0 < F; f0 += 4) {   // a quarter of the features at a time: registers
+        f32x4 v[4];
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = load4(x.v + min(n0 + 4 * g + e, x.M - 1) * x.v_row + ln * F + f0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (!(__builtin_fabsf(v[e][j]) < INFINITY)) { odd = true; v[e][j] = 0.f; }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          o[f0 + j] *= alpha;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[f0 + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][j], p[e], o[f0 + j], 0, 0, 0);
+        }
+        if (__builtin_amdgcn_ballot_w64(odd) != 0) {   // infinities and NaNs: for each row those of its own ancestors only
+#pragma unroll 1
+          for (int k = 0; k < 16; ++k) {
+            const float w = __shfl((k & 3) == 0 ? p[0] : (k & 3) == 1 ? p[1] : (k & 3) == 2 ? p[2] : p[3], ln + 16 * (k >> 2), 64);
+            if (!((mine >> k) & 1u)) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const f32x4 y = load4(x.v + (n0 + k) * x.v_row + (4 * g + e) * F + f0);
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (!(__builtin_fabsf(y[j]) < INFINITY)) o[f0 + j][e] += w * y[j];
+            }
+          }
+        }
+      }
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+  }
+};
+
+// OwnSums of the 16 rows from first_row on (p_rows and more: none) as a partial.  lds: kPathBytes; every thread of the workgroup comes here.
+template <int D, typename T>
+__device__ __forceinline__ void own_rows(const MxAttnArgs &a, unsigned char *lds, int kvh, int b, int first_row, int n_begin, int n_end, const T *q0, size_t part) {
+  const RootPaths paths(a, lds, b);
+  const OwnRows<T> x(a, kvh, b, D);
+  const int p_rows = a.group * x.M, row = first_row + (threadIdx.x & 15);
+  if (first_row >= p_rows) return;   // wave-uniform
+  const int pc = min(row, p_rows - 1), al = pc / x.M, node = pc - al * x.M;
+  const AncMask path = paths.of(node);
+  const OwnSums<D, T> sums(x, q0 + node * a.q.row + al * D, path, n_begin, n_end);
+  if (row >= p_rows) return;
+  if ((threadIdx.x & 63) < 16) {
+    a.part_m[part + row] = sums.m == -INFINITY && (path.lo | path.hi) == 0 ? -INFINITY : stored_max(sums.m);
+    a.part_l[part + row] = sums.l;
+  }
+  sums.store(a.part_o + (part + row) * D);
+}
+
+// The sums of a workgroup's R rows (KG groups of wavefronts) through LDS, whole rows to a partial; groups are added in ascending order.
+// lds: KG * R * (D + 6) floats, free.
+template <int D, int RB, int R, int KG, int NT, typename T, int NP>
+__device__ __forceinline__ void write_partial(const MxAttnArgs &a, const QueryRows<D, RB, T, NP> &x, float *lds, int kg, int wave_row, int row0, int p_rows, size_t part) {
+  constexpr int LD = D + 4, NV = D / 64;
+  const int lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
+  float *s_m = lds + KG * R * LD, *s_l = s_m + KG * R;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int r = kg * R + wave_row + rb * 16 + ln;
+    if (g == 0) { s_m[r] = x.r[rb]; s_l[r] = x.o[rb][4 * NV][0]; }
+    float *row = lds + (size_t)r * LD + 16 * g;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) *(f32x4 *)(row + 64 * i + 4 * q) = f32x4{x.o[rb][4 * i][q], x.o[rb][4 * i + 1][q], x.o[rb][4 * i + 2][q], x.o[rb][4 * i + 3][q]};
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < min(R, p_rows - row0) * (D / 4); i += NT) {
+    const int r = i / (D / 4), f = i % (D / 4) * 4;
+    float m = s_m[r], l, w[KG];
+#pragma unroll
+    for (int k = 1; k < KG; ++k) m = fmaxf(m, s_m[k * R + r]);
+    f32x4 v;
+    if constexpr (KG == 1) {
+      l = s_l[r];
+      v = *(const f32x4 *)(lds + (size_t)r * LD + f);
+    } else {
+      const float m_safe = m == -INFINITY ? 0.f : m;
+      l = 0.f;
+      v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KG; ++k) {
+        w[k] = __builtin_amdgcn_exp2f(s_m[k * R + r] - m_safe);   // 0 for a group without keys
+        l += s_l[k * R + r] * w[k];
+        v += *(const f32x4 *)(lds + (size_t)(k * R + r) * LD + f) * w[k];
+      }
+    }
+    if (f == 0) {
+      a.part_m[part + row0 + r] = stored_max(m);
+      a.part_l[part + row0 + r] = l;
+    }
+    *(f32x4 *)(a.part_o + (part + row0 + r) * D + f) = v;
+  }
+}
+
+// an empty split's partial is neutral
+template <int R>
+__device__ __forceinline__ void empty_partial(const MxAttnArgs &a, int row0, int p_rows, size_t part) {
+  for (int r = threadIdx.x; r < min(R, p_rows - row0); r += blockDim.x) {
+    a.part_m[part + row0 + r] = -INFINITY;
+    a.part_l[part + row0 + r] = 0.f;
+  }
+}
+
+// the workgroup behind all others stores the nodes' rows, which nobody reads here
+template <int D, int NW, typename T>
+__device__ __forceinline__ void append_rows(const MxAttnArgs &a, int kvh, int b) {
+  const int wave = threadIdx.x >> 6, ctx = a.ctx.v[b];
+  const OwnRows<T> x(a, kvh, b, D);
+  for (int i = (ctx / kMxGroup + wave) * kMxGroup; i < ctx + x.M; i += NW * kMxGroup) mx_store_group<D, T>(a.c, b, kvh, i, ctx, x.M, x.k, x.k_row, x.v, x.v_row);
+}
+
+constexpr int max_bytes(int a, int b) { return a > b ? a : b; }
+// the low `left` bits of eight
+__device__ __forceinline__ uint32_t low_bits(int left) { return left <= 0 ? 0u : (left >= 8 ? 255u : (1u << left) - 1); }
 
 }  // namespace
 
-// RB blocks of 16 query rows a wavefront, RW wavefronts side by side hold the rows of a workgroup and the KG = 4 / RW groups of
-// them take every KG-th run of 32 keys; the groups' sums meet in LDS at the end.  Workgroups before the splits take a block of
-// 32 draft nodes each; behind them one more a (sequence, kv head) stores the nodes' rows (APPEND), which no other reads.
-template <int D, int RB, int RW, typename T, bool PAGED>
-__global__ __launch_bounds__(256, RB == 1 ? (D == 128 && Parts<T>::N == 2 ? 3 : 4) : (RB == 2 ? 2 : 1)) void k_mx_attn(MxAttnArgs a) {
-  constexpr int KG = 4 / RW, NP = Parts<T>::N, R = 16 * RB * RW, ST = D / 32, NV = D / 64, LD = D + 4;
-  constexpr int kMergeBytes = KG > 1 ? 4 * 16 * RB * LD * 4 : 16, kDraftBytes = 4 * 4096 + kMaxNodes * 20;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[kMergeBytes > kDraftBytes ? kMergeBytes : kDraftBytes];
-  __shared__ float s_m[KG][R], s_l[KG][R];
-  const int kvh = blockIdx.y, b = blockIdx.z / a.n_row_groups, rg = blockIdx.z - b * a.n_row_groups;
-  const int lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
+// RB blocks of 16 query rows a wavefront; RW wavefronts side by side hold the rows of a workgroup, and the KG = 4 / RW groups of them take every KG-th run
+// of 32 keys, straight from the cache to registers; the groups' sums meet in LDS at the end.  Grid: (sequence and kv head, rows, part).  The first n_own parts
+// take the draft nodes, so that the splits behind fill in as those end (four sequences of 60 nodes over 16384 keys: 82 us, 109 with them last); a part behind all
+// others stores the nodes' rows.  Row groups of the same keys land on one XCD wherever sequences times kv heads are a multiple of 8.
+template <int D, int RB, int RW, typename T, int NP, bool PAGED>
+__global__ __launch_bounds__(256, RB > 1 ? 2 : (D == 128 && NP > 1 ? 3 : 4)) void k_mx_attn(MxAttnArgs a) {
+  constexpr int KG = 4 / RW, R = 16 * RB * RW, ST = D / 32, NV = D / 64, kUnit = 32 * KG;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[max_bytes(KG * R * (D + 6) * 4, kPathBytes)];
+  const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv, rg = blockIdx.y, lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rw = wave % RW, kg = wave / RW;
-  const int M = a.n_nodes, p_rows = a.group * M, n_parts = a.n_splits + a.n_draft;
-  const size_t part0 = ((size_t)b * a.c.n_kv + kvh) * n_parts;
+  const int p_rows = a.group * a.n_nodes, split = (int)blockIdx.z - a.n_own, row0 = rg * R, n_parts = a.n_splits + a.n_own;
+  const size_t part = (((size_t)b * a.c.n_kv + kvh) * n_parts + (split < 0 ? n_parts + split : split)) * p_rows;
   const T *q0 = (const T *)a.q.p + b * a.q.seq + kvh * a.group * D;
-  const int ctx = a.ctx.v[b];
-
-  if ((int)blockIdx.x < a.n_draft) {
-    // ---- a block of draft nodes: whole 32-row blocks of this row group
-    uint64_t *lo = (uint64_t *)(lds + 4 * 4096), *hi = lo + kMaxNodes;
-    int32_t *up = (int32_t *)(hi + kMaxNodes);
-    if (!a.anc && !a.chain) {   // root paths from the parents: every node takes over what lies above it, twice as far each time
-      const int i = threadIdx.x;
-      if (i < M) {
-        AncMask m = {0, 0};
-        m.set(i);
-        lo[i] = m.lo; hi[i] = m.hi;
-        up[i] = a.parent[b * M + i];
-      }
-      __syncthreads();
-      for (int far = 1; far < M; far *= 2) {
-        uint64_t l = 0, h = 0;
-        int32_t u = 0;
-        if (i < M) { u = up[i]; l = lo[i] | lo[u]; h = hi[i] | hi[u]; u = up[u]; }
-        __syncthreads();
-        if (i < M) { lo[i] = l; hi[i] = h; up[i] = u; }
-        __syncthreads();
-      }
-    }
-    auto mask_of = [&](int node) {
-      if (a.anc) return a.anc[b * M + node];
-      if (a.chain) return AncMask{node < 63 ? (2ull << node) - 1 : ~0ull, node < 64 ? 0ull : (node < 127 ? (2ull << (node - 64)) - 1 : ~0ull)};
-      return AncMask{lo[node], hi[node]};
-    };
-    const DraftRows<T> src = {q0, (const T *)a.k.p + b * a.k.seq + kvh * D, (const T *)a.v.p + b * a.v.seq + kvh * D, a.q.row, a.k.row, a.v.row};
-    const size_t row = (part0 + a.n_splits + blockIdx.x) * p_rows;
-    if constexpr (R == 16) {
-      if (wave == 0) draft_partial_small<D, T>(src, mask_of, M, a.group, a.part_m + row, a.part_l + row, a.part_o + row * D, (float *)lds);
-    } else
-      for (int rb = rg * R / 32 + wave; rb * 32 < min((rg + 1) * R, p_rows); rb += 4)
-        draft_partial<D>(src, mask_of, M, a.group, blockIdx.x, rb, a.part_m + row, a.part_l + row, a.part_o + row * D, (float *)lds + wave * 1024);
-    return;
+  if (split < 0) {   // first of all: the others fill in as these end
+    const int n0 = (-1 - split) * kMxOwnNodes;
+    return own_rows<D, T>(a, lds, kvh, b, wave * 16 < R ? row0 + wave * 16 : p_rows, n0, min(n0 + kMxOwnNodes, a.n_nodes), q0, part);
   }
-  const int split = blockIdx.x - a.n_draft;
   if (split >= a.n_splits) {
-    if (rg == 0)
-      for (int i = (ctx / kMxGroup + wave) * kMxGroup; i < ctx + M; i += 4 * kMxGroup)
-        mx_store_group<D, T>(a.c, b, kvh, i, ctx, M, (const T *)a.k.p + b * a.k.seq + kvh * D, a.k.row, (const T *)a.v.p + b * a.v.seq + kvh * D, a.v.row);
+    if (rg == 0) append_rows<D, 4, T>(a, kvh, b);
     return;
   }
-
-  const size_t part = (part0 + split) * p_rows;
-  const int k_begin = split * a.keys_per_split, k_end = min(ctx, k_begin + a.keys_per_split);
-  const int row0 = rg * R;
-  if (k_begin >= k_end) {   // empty split: neutral partial
-    for (int r = threadIdx.x; r < min(R, p_rows - row0); r += 256) {
-      a.part_m[part + row0 + r] = -INFINITY;
-      a.part_l[part + row0 + r] = 0.f;
-    }
-    return;
-  }
+  const int ctx = a.ctx.v[b], keys = (ctx + a.n_splits * kUnit - 1) / (a.n_splits * kUnit) * kUnit;   // each sequence's own share
+  const int k_begin = split * keys, k_end = min(ctx, k_begin + keys);
+  if (k_begin >= k_end) return empty_partial<R>(a, row0, p_rows, part);
 
   // past the end a wavefront reads the split's last keys again and leaves all of them out
-  const int last = (k_end - 1) & ~31;
+  const int first = k_begin + kg * 32, last = (k_end - 1) & ~31;
   KeyCodes<D> kc;
   ValueCodes<D> vc;
-  size_t r_next = a.c.block(b, kvh, min(k_begin + kg * 32, last));
-  auto load_k = [&](int k0, size_t r) {
-    const int s = PAGED ? k0 % kKvPage : k0;
+  size_t r = a.c.block(b, kvh, min(first, last));
+  auto at = [&](int k0) { return PAGED ? k0 % kKvPage : k0; };
+  kc.load(a.c, r, at(min(first, last)), ln, g);
+  vc.load(a.c, r, at(min(first, last)), ln, g);
+  if (PAGED) r = a.c.block(b, kvh, min(first + 32 * KG, last));
+  QueryRows<D, RB, T, NP> x;
+  x.start(a, q0, row0 + rw * RB * 16, p_rows, ln, g);
+  if (row0 + rw * RB * 16 < p_rows)   // wave-uniform
+    for (int k0 = first; k0 < k_end; k0 += 32 * KG) {
+      const int next = at(min(k0 + 32 * KG, last));
+      f32x4 s[RB][2];
+      x.clear(s);
+      bf16x8 kf[ST][2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int at = s + 8 * (ln >> 2) + 4 * t + (ln & 3);
-      const uint8_t *p = a.c.k_codes + MxOffsets<D>::k_codes(a.c, r, at) + g * (D / 8);
-      if constexpr (D == 128) {
-        const u32x4 w = *(const u32x4 *)p;
+      for (int i = 0; i < ST; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) kc.w[t][i] = w[i];
-      } else {
-        const u32x2 w = *(const u32x2 *)p;
-        kc.w[t][0] = w[0]; kc.w[t][1] = w[1];
+        for (int t = 0; t < 2; ++t) kf[i][t] = kc.operand(t, i);
+      kc.load(a.c, r, next, ln, g);
+#pragma unroll
+      for (int i = 0; i < ST; ++i) x.score(s, kf[i][0], kf[i][1], i);
+      if (k0 + 32 > k_end) {   // wave-uniform: the keys end in here
+        const int left = k_end - (k0 + 8 * g);
+        vc.keep(left);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) x.mask(s[rb], low_bits(left));
       }
-      kc.scale[t] = a.c.k_scales[MxOffsets<D>::k_scales(a.c, r, at) + g * (D / 32) / 4];
-    }
-  };
-  auto load_v = [&](int k0, size_t r) {
-    const int s = (PAGED ? k0 % kKvPage : k0) + 8 * g;
-    const uint8_t *p = a.c.v_codes + MxOffsets<D>::v_codes(a.c, r, s) + ln * 16;
-    const uint8_t *ps = a.c.v_scales + MxOffsets<D>::v_scales(a.c, r, s) + (ln >> 3) * 8;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      vc.w[i] = *(const u32x4 *)(p + 256 * i);
-      vc.scale[i] = *(const u32x2 *)(ps + 16 * i);
-    }
-  };
-  const int first = k_begin + kg * 32;
-  size_t r_v = r_next;
-  load_k(min(first, last), r_next);
-  load_v(min(first, last), r_v);
-  if (PAGED) r_next = a.c.block(b, kvh, min(first + 32 * KG, last));
-
-  // ---- queries: lane (ln, g) features (D / 4) g + 8 t .. of row ln of each block
-  bf16x8 qf[RB][ST][NP];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int pc = min(row0 + (rw * RB + rb) * 16 + ln, p_rows - 1), al = pc / M, node = pc - al * M;
-    const T *q = q0 + node * a.q.row + al * D + g * (D / 4);
-#pragma unroll
-    for (int t = 0; t < ST; ++t) query_parts(q + 8 * t, qf[rb][t]);
-  }
-
-  const float c = 1.44269504088896f / sqrtf((float)D);   // scores in powers of two
-  float m_run[RB], l_run[RB];
-  f32x4 o[RB][4 * NV];   // o[rb][4 i + j][r]: feature 64 i + 16 g + 4 r + j of row ln
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    m_run[rb] = -INFINITY;
-    l_run[rb] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4 * NV; ++i) o[rb][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  const bool rows_here = row0 + rw * RB * 16 < p_rows;   // wave-uniform
-  if (rows_here)
-  for (int k0 = first; k0 < k_end; k0 += 32 * KG) {
-    const int next = min(k0 + 32 * KG, last);
-    f32x4 s[RB][2];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) s[rb][0] = s[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    bf16x8 kf[2][ST];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < ST; ++i) kf[t][i] = mx_values(kc.w[t][i], mx_scale(kc.scale[t], 0));
-    load_k(next, r_next);
-#pragma unroll
-    for (int i = 0; i < ST; ++i)
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) s[rb][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][i], qf[rb][i][p], s[rb][t], 0, 0, 0);
-    const bool ragged = k0 + 32 > k_end;   // the keys end in here
-    if (ragged) {
-      const int left = k_end - (k0 + 8 * g);   // of this lane's eight keys
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e >= left) s[rb][e >> 2][e & 3] = -INFINITY;
-      // values behind the end: element 0 of the smallest scale, whatever lies there
-      const uint64_t keep = left <= 0 ? 0 : (left >= 8 ? ~0ull : (1ull << (8 * left)) - 1);
+      bf16x8 pf[RB][NP];
+      x.settle(s, pf, x.weigh(s, pf));
+      x.add(x.ones(), pf, 4 * NV);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        vc.scale[i][0] &= (uint32_t)keep;
-        vc.scale[i][1] &= (uint32_t)(keep >> 32);
+        bf16x8 vf[4];
+        vc.operands(i, vf);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) vc.w[i][w] &= (2 * w < left ? 0xffffu : 0u) | (2 * w + 1 < left ? 0xffff0000u : 0u);
+        for (int j = 0; j < 4; ++j) x.add(vf[j], pf, 4 * i + j);
       }
+      vc.load(a.c, r, next, ln, g);
+      if (PAGED) r = a.c.block(b, kvh, min(k0 + 64 * KG, last));
     }
-    bf16x8 pf[RB][NP];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      float top = fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3]));
-      top = fmaxf(top, fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3])));
-      if (__builtin_amdgcn_ballot_w64(top > m_run[rb]) != 0) {   // the largest score of some row so far: rare on long contexts
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float m_new = fmaxf(m_run[rb], top);
-        const float alpha = __builtin_amdgcn_exp2f((m_run[rb] - (m_new == -INFINITY ? 0.f : m_new)) * c);   // 0 at first
-        m_run[rb] = m_new;
-        l_run[rb] *= alpha;
-#pragma unroll
-        for (int i = 0; i < 4 * NV; ++i) o[rb][i] *= alpha;
-      }
-      const float ref = m_run[rb] == -INFINITY ? 0.f : m_run[rb] * c;
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const f32x2 p = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][e >> 2][e & 3], c, -ref)),
-                         __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][e >> 2][(e & 3) + 1], c, -ref))};   // 0 behind the end
-        l_run[rb] += p[0] + p[1];
-        prob_parts(p, pf[rb], e);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      uint32_t vf[4][4];   // [feature][pair of keys]
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t x = vc.w[i][w];
-        const float s0 = mx_scale(vc.scale[i][w >> 1], (2 * w) & 3), s1 = mx_scale(vc.scale[i][w >> 1], (2 * w + 1) & 3);
-        union { bf16x2 v; uint32_t u; } a0, a1, b0, b1;   // features 0, 1 and 2, 3 of both keys
-        a0.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s0, 0); a1.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s1, 2);
-        b0.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s0, 1); b1.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s1, 3);
-        vf[0][w] = __builtin_amdgcn_perm(a1.u, a0.u, 0x05040100); vf[1][w] = __builtin_amdgcn_perm(a1.u, a0.u, 0x07060302);
-        vf[2][w] = __builtin_amdgcn_perm(b1.u, b0.u, 0x05040100); vf[3][w] = __builtin_amdgcn_perm(b1.u, b0.u, 0x07060302);
-      }
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            o[rb][4 * i + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 *)vf[j], pf[rb][p], o[rb][4 * i + j], 0, 0, 0);
-    }
-    load_v(next, r_next);
-    if (PAGED) r_next = a.c.block(b, kvh, min(k0 + 64 * KG, last));
-  }
-
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    l_run[rb] += __shfl_xor(l_run[rb], 16, 64);
-    l_run[rb] += __shfl_xor(l_run[rb], 32, 64);
-  }
-  if constexpr (KG == 1) {
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int row = row0 + (rw * RB + rb) * 16 + ln;
-      if (row >= p_rows) continue;
-      if (g == 0) {
-        a.part_m[part + row] = stored_max(m_run[rb] * c);
-        a.part_l[part + row] = l_run[rb];
-      }
-      float *out = a.part_o + (part + row) * D + 16 * g;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          *(f32x4 *)(out + 64 * i + 4 * r) = f32x4{o[rb][4 * i][r], o[rb][4 * i + 1][r], o[rb][4 * i + 2][r], o[rb][4 * i + 3][r]};
-    }
-  } else {
-    // ---- the key groups' sums through LDS, added in ascending order; a thread then takes four features of some rows
-    float *so = (float *)lds;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      if (g == 0) { s_m[kg][(rw * RB + rb) * 16 + ln] = m_run[rb]; s_l[kg][(rw * RB + rb) * 16 + ln] = l_run[rb]; }
-      float *w = so + (size_t)(kg * R + (rw * RB + rb) * 16 + ln) * LD + 16 * g;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          *(f32x4 *)(w + 64 * i + 4 * r) = f32x4{o[rb][4 * i][r], o[rb][4 * i + 1][r], o[rb][4 * i + 2][r], o[rb][4 * i + 3][r]};
-    }
-    __syncthreads();
-    for (int x = threadIdx.x; x < min(R, p_rows - row0) * (D / 4); x += 256) {
-      const int r = x / (D / 4), f = x % (D / 4) * 4;
-      float m = -INFINITY, l = 0.f;
-#pragma unroll
-      for (int i = 0; i < KG; ++i) m = fmaxf(m, s_m[i][r]);
-      const float m_safe = m == -INFINITY ? 0.f : m;
-      f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < KG; ++i) {
-        const float w = __builtin_amdgcn_exp2f((s_m[i][r] - m_safe) * c);   // 0 for a group without keys
-        l += s_l[i][r] * w;
-        v += *(const f32x4 *)(so + (size_t)(i * R + r) * LD + f) * w;
-      }
-      if (f == 0) {
-        a.part_m[part + row0 + r] = stored_max(m * c);
-        a.part_l[part + row0 + r] = l;
-      }
-      *(f32x4 *)(a.part_o + (part + row0 + r) * D + f) = v;
-    }
-  }
+  write_partial<D, RB, R, KG, 256, T, NP>(a, x, (float *)lds, kg, rw * RB * 16, row0, p_rows, part);
 }
 
 namespace {
 enum { kOutPanels, kOutF32, kOutBf16 };
 }
 
-// Combine the partials of one (row, kv head) in ascending order, as k_attn_merge.  A row that saw no key at all (no context, no
-// nodes of its own) is 0.
+// Join the partials of a row and kv head.  A wavefront takes 64 features of a head, four a lane, and a quarter of the partials on every 16 lanes, all
+// of them requested at once: the time is that of one read, not of one behind another.  The quarters are joined as the partials are, in a fixed order.  A row that saw
+// no key at all (no context, no nodes of its own) is 0.
 template <int D, int NB, int OUT>
-__global__ __launch_bounds__(512) void k_mx_merge(MxAttnArgs a) {
-  const int r = blockIdx.x, kvh = blockIdx.y, tid = threadIdx.x;
-  const int M = a.n_nodes, group = a.group, b = r / M, node = r - b * M;
-  const int p_rows = group * M, n = a.n_splits + a.n_draft;
-  const size_t base = ((size_t)b * a.c.n_kv + kvh) * n;
-  const int al = tid / (D / 2), f = (tid - al * (D / 2)) * 2;   // head, first feature
-  if (al >= group) return;
-  const int p = al * M + node;
-  float num0 = 0.f, num1 = 0.f, den = 0.f;
+__global__ __launch_bounds__(1024) void k_mx_merge(MxAttnArgs a) {
+  const int r = blockIdx.x, kvh = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int M = a.n_nodes, b = r / M, node = r - b * M, p_rows = a.group * M, n = a.n_splits + a.n_own;
+  const int al = wave / (D / 64), f = (wave & (D / 64 - 1)) * 64 + (lane & 15) * 4, quarter = lane >> 4;
+  const size_t first = ((size_t)b * a.c.n_kv + kvh) * n * p_rows + al * M + node;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
   if (n > 0) {
     float pm[NB], pl[NB];
-    float2 po[NB];
-    auto request = [&](int s0) {
+    f32x4 po[NB];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const size_t idx = (base + min(s0 + i, n - 1)) * p_rows + p;
-        pm[i] = a.part_m[idx];
-        pl[i] = a.part_l[idx];
-        po[i] = *(const float2 *)(a.part_o + idx * D + f);
-      }
-    };
-    request(0);
-    float m_tot = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < NB; ++i) m_tot = fmaxf(m_tot, i < n ? pm[i] : -INFINITY);
-    for (int s0 = NB; s0 < n; s0 += 16) {   // many splits only
-      float t[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) t[i] = a.part_m[(base + min(s0 + i, n - 1)) * p_rows + p];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) m_tot = fmaxf(m_tot, t[i]);
+    for (int i = 0; i < NB; ++i) {
+      const size_t idx = first + (size_t)min(quarter + 4 * i, n - 1) * p_rows;
+      pm[i] = a.part_m[idx];
+      pl[i] = a.part_l[idx];
+      po[i] = *(const f32x4 *)(a.part_o + idx * D + f);
     }
-    for (int s0 = 0; s0 < n; s0 += NB) {
-      if (s0 > 0) request(s0);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        if (s0 + i >= n || pm[i] == -INFINITY) continue;   // no key in it: its o was never written
-        const float w = fast_exp(pm[i] - m_tot);
-        num0 += po[i].x * w;
-        num1 += po[i].y * w;
-        den += pl[i] * w;
-      }
+    for (int i = 0; i < NB; ++i) m = fmaxf(m, quarter + 4 * i < n ? pm[i] : -INFINITY);
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      if (quarter + 4 * i >= n || pm[i] == -INFINITY) continue;   // no key in it: its o was never written
+      const float w = __builtin_amdgcn_exp2f((pm[i] - m) * 1.44269504088896f);
+      o += po[i] * w;
+      l += pl[i] * w;
     }
-    if (m_tot == -INFINITY) den = 1.f;
-  } else {
-    den = 1.f;
+#pragma unroll
+    for (int x = 16; x < 64; x *= 2) {
+      l += __shfl_xor(l, x, 64);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], x, 64);
+    }
   }
-  const float o0 = num0 / den, o1 = num1 / den;
-  const int kk = (kvh * group + al) * D + f;
-  if constexpr (OUT == kOutPanels) {   // operand layout of the O projection; both features sit in the same 8-element run
-    const bf16 h0 = (bf16)o0, h1 = (bf16)o1;
-    bf16 *d0 = (bf16 *)a.out + ol_offset(r, kk, 0, (int)a.out_panel), *d1 = (bf16 *)a.out + ol_offset(r, kk, 1, (int)a.out_panel);
-    d0[0] = h0; d0[1] = h1;
-    d1[0] = (bf16)(o0 - (float)h0); d1[1] = (bf16)(o1 - (float)h1);
-  } else if constexpr (OUT == kOutF32) {
-    *(float2 *)((float *)a.out + r * a.out_row + kk) = float2{o0, o1};
+  const float den = m == -INFINITY ? 1.f : l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = o[e] / den;
+  const int kk = (kvh * a.group + al) * D + f;
+  if constexpr (OUT == kOutPanels) {   // operand layout of the O projection, where four features lie side by side
+    if (quarter > 1) return;
+    bf16x4 h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      h[e] = (bf16)o[e];
+      if (quarter == 1) h[e] = (bf16)(o[e] - (float)h[e]);
+    }
+    *(bf16x4 *)((bf16 *)a.out + ol_offset(r, kk, quarter, (int)a.out_panel)) = h;
   } else {
-    *(bf16x2 *)((bf16 *)a.out + r * a.out_row + kk) = bf16x2{(bf16)o0, (bf16)o1};
+    if (quarter > 0) return;
+    if constexpr (OUT == kOutF32) {
+      *(f32x4 *)((float *)a.out + r * a.out_row + kk) = o;
+    } else {
+      *(bf16x4 *)((bf16 *)a.out + r * a.out_row + kk) = bf16x4{(bf16)o[0], (bf16)o[1], (bf16)o[2], (bf16)o[3]};
+    }
   }
 }
 
 namespace {
 template <int D, int OUT>
 void launch_merge(hipStream_t st, const MxAttnArgs &a) {
-  const int threads = a.group * D / 2 < 64 ? 64 : a.group * D / 2;   // <= 512 (group <= 8, d <= 128)
-  const dim3 grid(a.batch * a.n_nodes, a.c.n_kv);
-  const int n = a.n_splits + a.n_draft;
-  if (n <= 6) hipLaunchKernelGGL((k_mx_merge<D, 6, OUT>), grid, dim3(threads), 0, st, a);
-  else if (n <= 12) hipLaunchKernelGGL((k_mx_merge<D, 12, OUT>), grid, dim3(threads), 0, st, a);
-  else hipLaunchKernelGGL((k_mx_merge<D, 20, OUT>), grid, dim3(threads), 0, st, a);
+  const dim3 grid(a.batch * a.n_nodes, a.c.n_kv), block(a.group * D);   // <= 1024 (group <= 8, d <= 128)
+  static_assert(4 * 16 >= kMaxAttnSplits, "every partial is read at once");
+  if (a.n_splits + a.n_own <= 4 * 4) hipLaunchKernelGGL((k_mx_merge<D, 4, OUT>), grid, block, 0, st, a);
+  else if (a.n_splits + a.n_own <= 4 * 8) hipLaunchKernelGGL((k_mx_merge<D, 8, OUT>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_mx_merge<D, 16, OUT>), grid, block, 0, st, a);
 }
 
-template <int D, typename T>
+template <int D, typename T, int NP>
 void launch_parts(hipStream_t st, const MxAttnArgs &a) {
-  const dim3 grid(a.n_draft + a.n_splits + (a.append ? 1 : 0), a.c.n_kv, a.batch * a.n_row_groups);
-  if (grid.x == 0) return;
-#define TS_MX(RB_, RW_)                                                                                                  \
-  do {                                                                                                                   \
-    if (a.c.page_table) hipLaunchKernelGGL((k_mx_attn<D, RB_, RW_, T, true>), grid, dim3(256), 0, st, a);                \
-    else hipLaunchKernelGGL((k_mx_attn<D, RB_, RW_, T, false>), grid, dim3(256), 0, st, a);                              \
+  const dim3 grid(a.batch * a.c.n_kv, a.n_row_groups, a.n_own + a.n_splits + (a.append ? 1 : 0));
+  if (grid.z == 0) return;   // no key anywhere
+#define TS_MX(KERNEL, THREADS, ...)                                                                                          \
+  do {                                                                                                              \
+    if (a.c.page_table) hipLaunchKernelGGL((KERNEL<D, __VA_ARGS__, true>), grid, dim3(THREADS), 0, st, a);          \
+    else hipLaunchKernelGGL((KERNEL<D, __VA_ARGS__, false>), grid, dim3(THREADS), 0, st, a);                        \
   } while (0)
-  const int form = a.row_blocks * 10 + a.row_waves;
-  if (form == 11) TS_MX(1, 1);
-  else if (form == 21) TS_MX(2, 1);
-  else if (form == 22) TS_MX(2, 2);
-  else if (form == 24) TS_MX(2, 4);
-  else TS_MX(4, 4);
+  if (a.form == kMxRows16) TS_MX(k_mx_attn, 256, 1, 1, T, NP);
+  else if (a.form == kMxRows32) TS_MX(k_mx_attn, 256, 2, 1, T, NP);
+  else TS_MX(k_mx_attn, 256, 2, 2, T, NP);
 #undef TS_MX
 }
 
 template <int D>
 void launch_d(hipStream_t st, const MxAttnArgs &a) {
-  if (a.dtype == TRISPEC_F32) launch_parts<D, float>(st, a); else launch_parts<D, bf16>(st, a);
-  if (a.out_row == 0) launch_merge<D, kOutPanels>(st, a);
-  else if (a.dtype == TRISPEC_F32) launch_merge<D, kOutF32>(st, a);
-  else launch_merge<D, kOutBf16>(st, a);
+  if (a.out_row == 0) {   // a verification pass
+    launch_parts<D, float, 2>(st, a);
+    launch_merge<D, kOutPanels>(st, a);
+  } else if (a.dtype == TRISPEC_F32) {
+    launch_parts<D, float, 3>(st, a);
+    launch_merge<D, kOutF32>(st, a);
+  } else {
+    launch_parts<D, bf16, 1>(st, a);
+    launch_merge<D, kOutBf16>(st, a);
+  }
 }
 }  // namespace
 

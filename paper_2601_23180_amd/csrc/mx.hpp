@@ -20,6 +20,12 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 
+__device__ __forceinline__ f32x4 load4(const float *p) { return *(const f32x4 *)p; }
+__device__ __forceinline__ f32x4 load4(const bf16 *p) {
+  const bf16x4 v = *(const bf16x4 *)p;
+  return f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+}
+
 constexpr int kMxBlock = 32;   // features that share a scale
 constexpr int kMxGroup = 8;    // slots whose values lie side by side
 
@@ -179,9 +185,9 @@ struct MxAttnArgs {
   int32_t chain;
   int32_t batch, n_nodes, n_q_heads, group, head_dim, dtype;
   int32_t append;             // the nodes' K and V go to slots ctx + i
-  int32_t row_blocks, row_waves;        // of 16 rows a wavefront, of wavefronts side by side
-  int32_t n_row_groups, keys_per_split, n_splits, n_draft;
-  float *part_o, *part_m, *part_l;   // as in AttnArgs, the draft blocks behind the splits
+  int32_t form;               // kMxRows*
+  int32_t n_row_groups, n_splits, n_own;
+  float *part_o, *part_m, *part_l;   // as in AttnArgs; n_own: the draft nodes have a partial of their own, else they are in the last split
   void *out;                  // rows [batch * n_nodes][n_q_heads * d] in dtype, or operand panels
   int64_t out_row;            // elements between rows; 0: operand panels of out_panel 32-row blocks
   size_t out_panel;

@@ -79,9 +79,9 @@ struct AttendLayout {
   size_t o, m, l, total;
 };
 AttendLayout attend_layout(int batch, int n_nodes, int group, int n_kv, int head_dim) {
-  // as many splits as the plan makes at most
-  const MxPlan p = plan_mx(batch, n_kv, group, n_nodes, true, 1l << 40);
-  const size_t rows = (size_t)batch * n_kv * (p.n_splits + p.n_draft) * group * n_nodes;
+  // as many splits as the plan makes at most: those of endless contexts, and those of the nodes
+  const MxPlan p = plan_mx(batch, n_kv, group, n_nodes, false, 1l << 30);
+  const size_t rows = (size_t)batch * n_kv * (p.n_splits + (n_nodes + kMxOwnNodes - 1) / kMxOwnNodes) * group * n_nodes;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   AttendLayout L;
   L.o = 0;
@@ -171,7 +171,7 @@ int trispec_mx_attend_workspace_bytes(int32_t batch, int32_t n_nodes, int32_t n_
   return TRISPEC_OK;
 }
 
-int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, const trispec_mx_attend_args *x) {
+int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, const int32_t *tree_parents, const trispec_mx_attend_args *x) {
   if (!c || !ctx_len_host || !x || !x->q.data || !x->out || !x->k.data != !x->v.data) return TRISPEC_ENULL;
   const bool own = x->k.data != nullptr;
   if (x->append && !own) return TRISPEC_ENULL;
@@ -194,10 +194,10 @@ int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, co
     a.ctx.v[b] = n;
     if (n > longest) longest = n;
   }
-  a.chain = x->tree_parents == nullptr;
-  if (x->tree_parents)
+  a.chain = tree_parents == nullptr;
+  if (tree_parents)
     for (int i = 0; i < B * M; ++i) {
-      const int node = i % M, p = x->tree_parents[i];
+      const int node = i % M, p = tree_parents[i];
       if (node == 0 ? p != -1 : (p < 0 || p >= node)) return TRISPEC_ETREE;
       a.parent[i] = (uint8_t)(node == 0 ? 0 : p);
     }
@@ -210,8 +210,8 @@ int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, co
   a.v = rows_of(x->v);
   a.batch = B; a.n_nodes = M; a.n_q_heads = x->n_q_heads; a.group = group; a.head_dim = D; a.dtype = x->dtype;
   a.append = x->append;
-  a.row_blocks = p.row_blocks; a.row_waves = p.row_waves; a.n_row_groups = p.n_row_groups;
-  a.keys_per_split = p.keys_per_split; a.n_splits = p.n_splits; a.n_draft = p.n_draft;
+  a.form = p.form; a.n_row_groups = p.n_row_groups;
+  a.n_splits = p.n_splits; a.n_own = p.n_own;
   char *ws = (char *)x->workspace;
   a.part_o = (float *)(ws + L.o);
   a.part_m = (float *)(ws + L.m);

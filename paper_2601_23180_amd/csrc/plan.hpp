@@ -335,28 +335,36 @@ inline AttnPlan plan_attn(int batch, int n_kv, int group, int head_dim, int n_no
   return best;
 }
 
-// ---- attention over the 4-bit cache (k_mx_attn): how query rows and keys are divided
+// ---- attention over the 4-bit cache: how query rows and keys are divided
+enum { kMxRows16 = 0, kMxRows32, kMxRows64 };   // rows of a workgroup
+constexpr int kMxOwnNodes = 32;                 // draft nodes of a partial
 struct MxPlan {
-  int row_blocks, row_waves, n_row_groups, keys_per_split, n_splits, n_draft;
+  int form, n_row_groups, n_splits, n_own;   // n_own: partials of the draft nodes, kMxOwnNodes each
 };
-// group * n_nodes query rows per kv head over up to max_keys keys
+// group * n_nodes query rows per kv head over up to max_keys keys.
+//
+// Rows: one block of 16 a wavefront up to 16 rows, else two, by one or two wavefronts side by side; larger workgroups, also ones that stage converted keys in
+// LDS, are no faster (60 nodes of 4 heads a kv head over 4096 keys, 128 rows a workgroup 18.5 us and 64 rows 15.2, 16384 keys of four sequences 86.3 and 85.7): what
+// bounds the kernel is the conversion beside the products, not the reading.
+// Splits: workgroups for every CU once, the nodes' own among them where they are few, over 256 keys at least; twice where a split would be longer than
+// 4096 keys, since two workgroups a CU hide each other's latencies.  us, context + merge, once / twice: 60 nodes, 4096 keys 16.0 + 4.0 / 19.4 + 5.1; 128
+// nodes, 8192 keys 32.8 + 5.3 / 33.3 + 6.5; four sequences of 60 nodes and 16384 keys 94.1 + 5.5 / 82.4 + 6.2; eight of one token and 32768 keys 55.5
+// / 46.2 (45.3 for 768 workgroups); one token of one sequence, 32768 keys 10.7 / 11.0, 4096 keys 5.5 / 6.1.
 inline MxPlan plan_mx(int batch, int n_kv, int group, int n_nodes, bool own_nodes, long max_keys) {
   const int p_rows = group * n_nodes;
   MxPlan p;
-  p.row_blocks = p_rows <= 16 ? 1 : (p_rows <= 128 ? 2 : 4);
-  p.row_waves = p_rows <= 32 ? 1 : (p_rows <= 64 ? 2 : 4);
-  const int rows = 16 * p.row_blocks * p.row_waves, groups = 4 / p.row_waves;
+  p.form = p_rows <= 16 ? kMxRows16 : p_rows <= 32 ? kMxRows32 : kMxRows64;
+  const int rows = 16 << p.form;
   p.n_row_groups = (p_rows + rows - 1) / rows;
-  p.n_draft = own_nodes ? (n_nodes + 31) / 32 : 0;
   const int per_split = batch * n_kv * p.n_row_groups;
-  int want = (p.row_blocks == 1 ? 1024 : (p.row_blocks == 2 ? 512 : 256)) / per_split;
-  if (want > kMaxAttnSplits) want = kMaxAttnSplits;
+  p.n_own = own_nodes ? (n_nodes + kMxOwnNodes - 1) / kMxOwnNodes : 0;
+  const int own = p.n_own * per_split;
+  const int room = (long)per_split * max_keys > 256 * 4096l ? 512 : own <= 64 ? 256 - own : 256;
+  int want = room / per_split;
+  if (want > kMaxAttnSplits - p.n_own) want = kMaxAttnSplits - p.n_own;
   if (want < 1) want = 1;
-  const int unit = 32 * groups;
-  long kps = ((max_keys + want - 1) / want + unit - 1) / unit * unit;
-  if (kps < 128) kps = 128;
-  p.n_splits = (int)((max_keys + kps - 1) / kps);
-  p.keys_per_split = (int)kps;
+  p.n_splits = (int)((max_keys + 255) / 256);
+  if (p.n_splits > want) p.n_splits = want;
   return p;
 }
 

@@ -91,13 +91,13 @@ def test_rows_are_checked_before_any_launch(which):
 def test_attention_is_checked_before_any_launch():
     lib = B.lib()
 
-    def call(c=None, ctx=ints(10, 20), **kw):
+    def call(c=None, ctx=ints(10, 20), tree_parents=None, **kw):
         c = c or desc()
-        base = dict(q=rows(row=1024), k=rows(), v=rows(), dtype=1, n_nodes=3, n_q_heads=8, tree_parents=None, append=0, out=0x70000,
+        base = dict(q=rows(row=1024), k=rows(), v=rows(), dtype=1, n_nodes=3, n_q_heads=8, append=0, out=0x70000,
                     out_row_stride=1024, workspace=0x80000, workspace_bytes=1 << 40, stream=None)
         base.update(kw)
         a = B.MXAttendArgs(*[base[k] for k, _ in B.MXAttendArgs._fields_])
-        return lib.trispec_mx_attend(C.byref(c), ctx, C.byref(a))
+        return lib.trispec_mx_attend(C.byref(c), ctx, tree_parents, C.byref(a))
 
     none = B.MXRows(None, 0, 0)
     assert call(q=none) == ENULL and call(k=none) == ENULL and call(v=none) == ENULL and call(out=None) == ENULL and call(ctx=None) == ENULL
