@@ -545,7 +545,7 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
   MxAttnArgs mx;
   memset(&mx, 0, sizeof(mx));
   if (kv->held_in_mx) {
-    const MxPlan p = plan_mx(B, c.n_kv_heads, group, n_nodes, true, max_keys);
+    const MxPlan p = plan_mx(B, c.n_kv_heads, group, n_nodes, true, true, max_keys);
     const float *rows_f32 = (const float *)(ws + L.qkv_f32);
     const int64_t seq = (int64_t)n_nodes * nqkv;
     mx.ctx = ctx;
@@ -556,7 +556,7 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
     mx.batch = B; mx.n_nodes = n_nodes; mx.n_q_heads = c.n_q_heads; mx.group = group; mx.head_dim = c.head_dim;
     mx.dtype = TRISPEC_F32;
     mx.append = 1;
-    mx.form = p.form; mx.n_row_groups = p.n_row_groups;
+    mx.whole = p.whole; mx.form = p.form; mx.n_row_groups = p.n_row_groups;
     mx.n_splits = p.n_splits; mx.n_own = p.n_own;
     mx.part_o = (float *)(ws + L.attn_o);
     mx.part_m = (float *)(ws + L.attn_m);

@@ -74,23 +74,22 @@ template <int D>
 struct KeyCodes {
   uint32_t w[2][D / 32];
   uint32_t scale[2];
+  // uniform bases and 32-bit lane offsets: the address arithmetic stays off the vector ALU
   __device__ __forceinline__ void load(const MxMap &m, size_t r, int s, uint32_t ln, uint32_t g) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) load(m, r, s, ln, g, t, t);
-  }
-  // run t's into place `to`.  Uniform bases and 32-bit lane offsets: the address arithmetic stays off the vector ALU
-  __device__ __forceinline__ void load(const MxMap &m, size_t r, int s, uint32_t ln, uint32_t g, int t, int to) {
-    const uint8_t *codes = m.k_codes + MxOffsets<D>::k_codes(m, r, s + 4 * t), *scales = m.k_scales + MxOffsets<D>::k_scales(m, r, s + 4 * t);
     const uint32_t at = 8 * (ln >> 2) + (ln & 3);
-    if constexpr (D == 128) {
-      const u32x4 x = *(const u32x4 *)(codes + (at * (D / 2) + g * (D / 8)));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[to][i] = x[i];
-    } else {
-      const u32x2 x = *(const u32x2 *)(codes + (at * (D / 2) + g * (D / 8)));
-      w[to][0] = x[0]; w[to][1] = x[1];
+    for (int t = 0; t < 2; ++t) {
+      const uint8_t *codes = m.k_codes + MxOffsets<D>::k_codes(m, r, s + 4 * t), *scales = m.k_scales + MxOffsets<D>::k_scales(m, r, s + 4 * t);
+      if constexpr (D == 128) {
+        const u32x4 x = *(const u32x4 *)(codes + (at * (D / 2) + g * (D / 8)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[t][i] = x[i];
+      } else {
+        const u32x2 x = *(const u32x2 *)(codes + (at * (D / 2) + g * (D / 8)));
+        w[t][0] = x[0]; w[t][1] = x[1];
+      }
+      scale[t] = scales[at * (D / 32) + g * (D / 32) / 4];
     }
-    scale[to] = scales[at * (D / 32) + g * (D / 32) / 4];
   }
   // operand of reduction step i for 16 keys: features (D / 4) g + 8 i ..
   __device__ __forceinline__ bf16x8 operand(int t, int i) const { return mx_values(w[t][i], mx_scale(scale[t], 0)); }
@@ -100,13 +99,12 @@ struct ValueCodes {
   u32x4 w[D / 64];
   u32x2 scale[D / 64];
   __device__ __forceinline__ void load(const MxMap &m, size_t r, int s, uint32_t ln, uint32_t g) {
+    const uint8_t *codes = m.v_codes + MxOffsets<D>::v_codes(m, r, s), *scales = m.v_scales + MxOffsets<D>::v_scales(m, r, s);
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) load(m, r, s, ln, g, i, i);
-  }
-  // the 64 features from 64 i on into place `to`
-  __device__ __forceinline__ void load(const MxMap &m, size_t r, int s, uint32_t ln, uint32_t g, int i, int to) {
-    w[to] = *(const u32x4 *)(m.v_codes + MxOffsets<D>::v_codes(m, r, s) + 256 * i + (g * (8 * D / 2) + ln * 16));
-    scale[to] = *(const u32x2 *)(m.v_scales + MxOffsets<D>::v_scales(m, r, s) + 16 * i + (g * (8 * D / 32) + (ln >> 3) * 8));
+    for (int i = 0; i < D / 64; ++i) {
+      w[i] = *(const u32x4 *)(codes + 256 * i + (g * (8 * D / 2) + ln * 16));
+      scale[i] = *(const u32x2 *)(scales + 16 * i + (g * (8 * D / 32) + (ln >> 3) * 8));
+    }
   }
   // only the first `left` of the lane's eight keys are tokens: the others become element 0 of the smallest scale, whatever lies there
   __device__ __forceinline__ void keep(int left) {
@@ -225,33 +223,23 @@ struct QueryRows {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) o[rb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb][p], o[rb][i], 0, 0, 0);
   }
+  // into LDS, rows from `row` on
+  __device__ __forceinline__ void store(float *lds, int ld, float *s_m, float *s_l, int row) const {
+    const int lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int to = row + rb * 16 + ln;
+      if (g == 0) { s_m[to] = r[rb]; s_l[to] = o[rb][NO][0]; }
+      float *p = lds + (size_t)to * ld + 16 * g;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *(f32x4 *)(p + 64 * i + 4 * q) = f32x4{o[rb][4 * i][q], o[rb][4 * i + 1][q], o[rb][4 * i + 2][q], o[rb][4 * i + 3][q]};
+    }
+  }
   static __device__ __forceinline__ bf16x8 ones() {
     const bf16 x = (bf16)1.f;
     return bf16x8{x, x, x, x, x, x, x, x};
-  }
-  // What infinities and NaNs among the values of the nodes 32 kb .. add to the rows that see them (sees).  They are left out of the products,
-  // where a weight of 0 would carry them into rows of other branches.
-  __device__ __forceinline__ void add_odd(const T *v, int64_t v_row, int kb, const uint32_t (&sees)[RB], const bf16x8 (&pf)[RB][NP]) {
-    const int lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
-#pragma unroll 1
-    for (int n = 0; n < 32; ++n)
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        float w = 0.f;   // of node n, in the lane that holds it
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w = (n & 7) == e ? (float)pf[rb][0][e] : w;
-        w = __shfl(w, ln + 16 * (n >> 3), 64);
-        if (!((sees[rb] >> n) & 1u)) continue;   // an ancestor is a node of the tree
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const f32x4 y = load4(v + (32 * kb + n) * v_row + 64 * i + 16 * g + 4 * e);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (!(__builtin_fabsf(y[j]) < INFINITY)) o[rb][4 * i + j][e] += w * y[j];
-          }
-      }
   }
 };
 
@@ -299,6 +287,28 @@ struct RootPaths {
     return AncMask{lo[node], hi[node]};
   }
 };
+
+enum { kOutPanels, kOutF32, kOutBf16, kPartials };
+// four features from kk on of result row r
+template <int OUT>
+__device__ __forceinline__ void store_result(const MxAttnArgs &a, int r, int kk, const f32x4 &o) {
+  if constexpr (OUT == kOutF32) {
+    *(f32x4 *)((float *)a.out + r * a.out_row + kk) = o;
+    return;
+  }
+  bf16x4 h;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h[e] = (bf16)o[e];
+  if constexpr (OUT == kOutBf16) {
+    *(bf16x4 *)((bf16 *)a.out + r * a.out_row + kk) = h;
+  } else {   // operand layout of the O projection, where they lie side by side
+    bf16x4 rest;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) rest[e] = (bf16)(o[e] - (float)h[e]);
+    *(bf16x4 *)((bf16 *)a.out + ol_offset(r, kk, 0, (int)a.out_panel)) = h;
+    *(bf16x4 *)((bf16 *)a.out + ol_offset(r, kk, 1, (int)a.out_panel)) = rest;
+  }
+}
 
 // Softmax sums of 16 query rows over draft nodes n_begin .. n_end, by one wavefront with 16 x 16 x 4 fp32 instructions, 16 nodes at a time.
 // Lane (ln, g): features D/4 g .. of node / query row ln for the scores, which come out as nodes 4 g + e of row ln; features D/16 ln .. of the
@@ -415,52 +425,6 @@ __device__ __forceinline__ void own_rows(const MxAttnArgs &a, unsigned char *lds
   sums.store(a.part_o + (part + row) * D);
 }
 
-// The sums of a workgroup's R rows (KG groups of wavefronts) through LDS, whole rows to a partial; groups are added in ascending order.
-// lds: KG * R * (D + 6) floats, free.
-template <int D, int RB, int R, int KG, int NT, typename T, int NP>
-__device__ __forceinline__ void write_partial(const MxAttnArgs &a, const QueryRows<D, RB, T, NP> &x, float *lds, int kg, int wave_row, int row0, int p_rows, size_t part) {
-  constexpr int LD = D + 4, NV = D / 64;
-  const int lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
-  float *s_m = lds + KG * R * LD, *s_l = s_m + KG * R;
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int r = kg * R + wave_row + rb * 16 + ln;
-    if (g == 0) { s_m[r] = x.r[rb]; s_l[r] = x.o[rb][4 * NV][0]; }
-    float *row = lds + (size_t)r * LD + 16 * g;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) *(f32x4 *)(row + 64 * i + 4 * q) = f32x4{x.o[rb][4 * i][q], x.o[rb][4 * i + 1][q], x.o[rb][4 * i + 2][q], x.o[rb][4 * i + 3][q]};
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < min(R, p_rows - row0) * (D / 4); i += NT) {
-    const int r = i / (D / 4), f = i % (D / 4) * 4;
-    float m = s_m[r], l, w[KG];
-#pragma unroll
-    for (int k = 1; k < KG; ++k) m = fmaxf(m, s_m[k * R + r]);
-    f32x4 v;
-    if constexpr (KG == 1) {
-      l = s_l[r];
-      v = *(const f32x4 *)(lds + (size_t)r * LD + f);
-    } else {
-      const float m_safe = m == -INFINITY ? 0.f : m;
-      l = 0.f;
-      v = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < KG; ++k) {
-        w[k] = __builtin_amdgcn_exp2f(s_m[k * R + r] - m_safe);   // 0 for a group without keys
-        l += s_l[k * R + r] * w[k];
-        v += *(const f32x4 *)(lds + (size_t)(k * R + r) * LD + f) * w[k];
-      }
-    }
-    if (f == 0) {
-      a.part_m[part + row0 + r] = stored_max(m);
-      a.part_l[part + row0 + r] = l;
-    }
-    *(f32x4 *)(a.part_o + (part + row0 + r) * D + f) = v;
-  }
-}
-
 // an empty split's partial is neutral
 template <int R>
 __device__ __forceinline__ void empty_partial(const MxAttnArgs &a, int row0, int p_rows, size_t part) {
@@ -478,85 +442,151 @@ __device__ __forceinline__ void append_rows(const MxAttnArgs &a, int kvh, int b)
   for (int i = (ctx / kMxGroup + wave) * kMxGroup; i < ctx + x.M; i += NW * kMxGroup) mx_store_group<D, T>(a.c, b, kvh, i, ctx, x.M, x.k, x.k_row, x.v, x.v_row);
 }
 
-constexpr int max_bytes(int a, int b) { return a > b ? a : b; }
 // the low `left` bits of eight
 __device__ __forceinline__ uint32_t low_bits(int left) { return left <= 0 ? 0u : (left >= 8 ? 255u : (1u << left) - 1); }
 
 }  // namespace
 
-// RB blocks of 16 query rows a wavefront; RW wavefronts side by side hold the rows of a workgroup, and the KG = 4 / RW groups of them take every KG-th run
-// of 32 keys, straight from the cache to registers; the groups' sums meet in LDS at the end.  Grid: (sequence and kv head, rows, part).  The first n_own parts
+// RB blocks of 16 query rows a wavefront; RW wavefronts side by side hold the rows of a workgroup, and KG groups of them take every KG-th run
+// of 32 keys, straight from the cache to registers; the groups' sums meet in LDS at the end.
+//
+// OUT = kPartials: four wavefronts; grid (sequence and kv head, rows, part).  The first n_own parts
 // take the draft nodes, so that the splits behind fill in as those end (four sequences of 60 nodes over 16384 keys: 82 us, 109 with them last); a part behind all
 // others stores the nodes' rows.  Row groups of the same keys land on one XCD wherever sequences times kv heads are a multiple of 8.
-template <int D, int RB, int RW, typename T, int NP, bool PAGED>
-__global__ __launch_bounds__(256, RB > 1 ? 2 : (D == 128 && NP > 1 ? 3 : 4)) void k_mx_attn(MxAttnArgs a) {
-  constexpr int KG = 4 / RW, R = 16 * RB * RW, ST = D / 32, NV = D / 64, kUnit = 32 * KG;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[max_bytes(KG * R * (D + 6) * 4, kPathBytes)];
-  const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv, rg = blockIdx.y, lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rw = wave % RW, kg = wave / RW;
-  const int p_rows = a.group * a.n_nodes, split = (int)blockIdx.z - a.n_own, row0 = rg * R, n_parts = a.n_splits + a.n_own;
+// Else: short contexts.  One workgroup of eight wavefronts takes its rows over all keys and nodes and writes their results, which saves the partials' way
+// through memory and the launch behind them; RB of the wavefronts take the draft nodes, 16 rows each.
+template <int D, int RB, int RW, typename T, int NP, int OUT, bool PAGED>
+__global__ __launch_bounds__(OUT == kPartials ? 256 : 512, OUT != kPartials || RB > 1 ? 2 : 3) void k_mx_attn(MxAttnArgs a) {
+  constexpr bool kWhole = OUT != kPartials;
+  constexpr int NW = kWhole ? 8 : 4, KG = kWhole ? 8 - RB : 4 / RW, R = 16 * RB * RW, ST = D / 32, NV = D / 64, kUnit = 32 * KG;
+  constexpr int LD = D + 4, kSums = kWhole ? KG + 1 : KG;   // rows of sums in LDS: those of the groups, then those of the nodes
+  __shared__ __attribute__((aligned(16))) float sums[kSums * R * LD];
+  __shared__ float s_m[kSums * R], s_l[kSums * R];
+  __shared__ __attribute__((aligned(16))) unsigned char path_lds[kWhole ? kPathBytes : 16];
+  const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv, row0 = blockIdx.y * R, lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rw = kWhole ? 0 : wave % RW, kg = kWhole ? wave - RB : wave / RW;
+  const int p_rows = a.group * a.n_nodes, split = (int)blockIdx.z - (kWhole ? 0 : a.n_own), n_parts = a.n_splits + a.n_own;
   const size_t part = (((size_t)b * a.c.n_kv + kvh) * n_parts + (split < 0 ? n_parts + split : split)) * p_rows;
   const T *q0 = (const T *)a.q.p + b * a.q.seq + kvh * a.group * D;
+  const int ctx = a.ctx.v[b], first_row = row0 + rw * RB * 16;
   if (split < 0) {   // first of all: the others fill in as these end
     const int n0 = (-1 - split) * kMxOwnNodes;
-    return own_rows<D, T>(a, lds, kvh, b, wave * 16 < R ? row0 + wave * 16 : p_rows, n0, min(n0 + kMxOwnNodes, a.n_nodes), q0, part);
+    static_assert(kWhole || sizeof(sums) >= kPathBytes, "the nodes' root paths lie there");
+    return own_rows<D, T>(a, (unsigned char *)sums, kvh, b, wave * 16 < R ? row0 + wave * 16 : p_rows, n0, min(n0 + kMxOwnNodes, a.n_nodes), q0, part);
   }
-  if (split >= a.n_splits) {
-    if (rg == 0) append_rows<D, 4, T>(a, kvh, b);
+  if (split >= (kWhole ? 1 : a.n_splits)) {
+    if (blockIdx.y == 0) append_rows<D, NW, T>(a, kvh, b);
     return;
   }
-  const int ctx = a.ctx.v[b], keys = (ctx + a.n_splits * kUnit - 1) / (a.n_splits * kUnit) * kUnit;   // each sequence's own share
-  const int k_begin = split * keys, k_end = min(ctx, k_begin + keys);
-  if (k_begin >= k_end) return empty_partial<R>(a, row0, p_rows, part);
-
-  // past the end a wavefront reads the split's last keys again and leaves all of them out
-  const int first = k_begin + kg * 32, last = (k_end - 1) & ~31;
-  KeyCodes<D> kc;
-  ValueCodes<D> vc;
-  size_t r = a.c.block(b, kvh, min(first, last));
-  auto at = [&](int k0) { return PAGED ? k0 % kKvPage : k0; };
-  kc.load(a.c, r, at(min(first, last)), ln, g);
-  vc.load(a.c, r, at(min(first, last)), ln, g);
-  if (PAGED) r = a.c.block(b, kvh, min(first + 32 * KG, last));
-  QueryRows<D, RB, T, NP> x;
-  x.start(a, q0, row0 + rw * RB * 16, p_rows, ln, g);
-  if (row0 + rw * RB * 16 < p_rows)   // wave-uniform
-    for (int k0 = first; k0 < k_end; k0 += 32 * KG) {
-      const int next = at(min(k0 + 32 * KG, last));
-      f32x4 s[RB][2];
-      x.clear(s);
-      bf16x8 kf[ST][2];
-#pragma unroll
-      for (int i = 0; i < ST; ++i)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) kf[i][t] = kc.operand(t, i);
-      kc.load(a.c, r, next, ln, g);
-#pragma unroll
-      for (int i = 0; i < ST; ++i) x.score(s, kf[i][0], kf[i][1], i);
-      if (k0 + 32 > k_end) {   // wave-uniform: the keys end in here
-        const int left = k_end - (k0 + 8 * g);
-        vc.keep(left);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) x.mask(s[rb], low_bits(left));
+  int k_begin = 0, k_end = ctx;
+  if (!kWhole) {   // each sequence's own share
+    const int keys = (ctx + a.n_splits * kUnit - 1) / (a.n_splits * kUnit) * kUnit;
+    k_begin = split * keys;
+    k_end = min(ctx, k_begin + keys);
+    if (k_begin >= k_end) return empty_partial<R>(a, row0, p_rows, part);
+  }
+  if constexpr (kWhole) {
+    const RootPaths paths(a, path_lds, b);
+    if (kg < 0) {
+      const int row = row0 + wave * 16, at = KG * R + wave * 16 + ln;
+      if (a.k.p && row < p_rows) {   // wave-uniform
+        const OwnRows<T> nodes(a, kvh, b, D);
+        const int pc = min(row + ln, p_rows - 1), al = pc / a.n_nodes, node = pc - al * a.n_nodes;
+        const OwnSums<D, T> own(nodes, q0 + node * a.q.row + al * D, paths.of(node), 0, a.n_nodes);
+        if (g == 0) { s_m[at] = own.m; s_l[at] = own.l; }
+        own.store(sums + at * LD);
+      } else if (g == 0) {
+        s_m[at] = -INFINITY;
       }
-      bf16x8 pf[RB][NP];
-      x.settle(s, pf, x.weigh(s, pf));
-      x.add(x.ones(), pf, 4 * NV);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        bf16x8 vf[4];
-        vc.operands(i, vf);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x.add(vf[j], pf, 4 * i + j);
-      }
-      vc.load(a.c, r, next, ln, g);
-      if (PAGED) r = a.c.block(b, kvh, min(k0 + 64 * KG, last));
+    } else if (kg * 32 >= ctx) {   // no run
+      for (int i = lane; i < R; i += 64) s_m[kg * R + i] = -INFINITY;
     }
-  write_partial<D, RB, R, KG, 256, T, NP>(a, x, (float *)lds, kg, rw * RB * 16, row0, p_rows, part);
-}
+  }
 
-namespace {
-enum { kOutPanels, kOutF32, kOutBf16 };
+  if (!kWhole || (kg >= 0 && kg * 32 < ctx)) {   // wave-uniform
+    // the codes of a run are requested where those of the run before are used; past the end the last keys are read again and left out
+    const int first = k_begin + kg * 32, last = (k_end - 1) & ~31;
+    KeyCodes<D> kc;
+    ValueCodes<D> vc;
+    size_t r = a.c.block(b, kvh, min(first, last));
+    auto at = [&](int k0) { return PAGED ? k0 % kKvPage : k0; };
+    kc.load(a.c, r, at(min(first, last)), ln, g);
+    vc.load(a.c, r, at(min(first, last)), ln, g);
+    if (PAGED) r = a.c.block(b, kvh, min(first + 32 * KG, last));
+    QueryRows<D, RB, T, NP> x;
+    x.start(a, q0, first_row, p_rows, ln, g);
+    if (first_row < p_rows)   // wave-uniform
+      for (int k0 = first; k0 < k_end; k0 += 32 * KG) {
+        const int next = at(min(k0 + 32 * KG, last));
+        f32x4 s[RB][2];
+        x.clear(s);
+        bf16x8 kf[ST][2];
+#pragma unroll
+        for (int i = 0; i < ST; ++i)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) kf[i][t] = kc.operand(t, i);
+        kc.load(a.c, r, next, ln, g);
+#pragma unroll
+        for (int i = 0; i < ST; ++i) x.score(s, kf[i][0], kf[i][1], i);
+        if (k0 + 32 > k_end) {   // wave-uniform: the keys end in here
+          const int left = k_end - (k0 + 8 * g);
+          vc.keep(left);
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) x.mask(s[rb], low_bits(left));
+        }
+        bf16x8 pf[RB][NP];
+        x.settle(s, pf, x.weigh(s, pf));
+        x.add(x.ones(), pf, 4 * NV);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          bf16x8 vf[4];
+          vc.operands(i, vf);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x.add(vf[j], pf, 4 * i + j);
+        }
+        vc.load(a.c, r, next, ln, g);
+        if (PAGED) r = a.c.block(b, kvh, min(k0 + 64 * KG, last));
+      }
+    x.store(sums, LD, s_m, s_l, kg * R + rw * RB * 16);
+  }
+  __syncthreads();
+
+  // whole rows, the groups in ascending order
+  for (int i = threadIdx.x; i < min(R, p_rows - row0) * (D / 4); i += 64 * NW) {
+    const int r = i / (D / 4), f = i % (D / 4) * 4;
+    float m = s_m[r], l = 0.f;
+#pragma unroll
+    for (int k = 1; k < kSums; ++k) m = fmaxf(m, s_m[k * R + r]);
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (kSums == 1) {
+      l = s_l[r];
+      o = *(const f32x4 *)(sums + r * LD + f);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kSums; ++k) {
+        // nothing there (or scores of -infinity, which weigh nothing)
+        const float mk = s_m[k * R + r], lk = s_l[k * R + r], w = __builtin_amdgcn_exp2f(mk - m);
+        const f32x4 ok = *(const f32x4 *)(sums + (k * R + r) * LD + f);
+        const bool some = mk != -INFINITY;
+        l += some ? lk * w : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += some ? ok[e] * w : 0.f;
+      }
+    }
+    if constexpr (kWhole) {
+      const int al = (row0 + r) / a.n_nodes, node = row0 + r - al * a.n_nodes;
+      const float den = ctx > 0 || a.k.p ? l : 1.f;   // no key at all: 0
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = o[e] / den;
+      store_result<OUT>(a, b * a.n_nodes + node, (kvh * a.group + al) * D + f, o);
+    } else {
+      if (f == 0) {
+        a.part_m[part + row0 + r] = stored_max(m);
+        a.part_l[part + row0 + r] = l;
+      }
+      *(f32x4 *)(a.part_o + (part + row0 + r) * D + f) = o;
+    }
+  }
 }
 
 // Join the partials of a row and kv head.  A wavefront takes 64 features of a head, four a lane, and a quarter of the partials on every 16 lanes, all
@@ -601,24 +631,7 @@ __global__ __launch_bounds__(1024) void k_mx_merge(MxAttnArgs a) {
   const float den = m == -INFINITY ? 1.f : l;
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = o[e] / den;
-  const int kk = (kvh * a.group + al) * D + f;
-  if constexpr (OUT == kOutPanels) {   // operand layout of the O projection, where four features lie side by side
-    if (quarter > 1) return;
-    bf16x4 h;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      h[e] = (bf16)o[e];
-      if (quarter == 1) h[e] = (bf16)(o[e] - (float)h[e]);
-    }
-    *(bf16x4 *)((bf16 *)a.out + ol_offset(r, kk, quarter, (int)a.out_panel)) = h;
-  } else {
-    if (quarter > 0) return;
-    if constexpr (OUT == kOutF32) {
-      *(f32x4 *)((float *)a.out + r * a.out_row + kk) = o;
-    } else {
-      *(bf16x4 *)((bf16 *)a.out + r * a.out_row + kk) = bf16x4{(bf16)o[0], (bf16)o[1], (bf16)o[2], (bf16)o[3]};
-    }
-  }
+  if (quarter == 0) store_result<OUT>(a, r, (kvh * a.group + al) * D + f, o);
 }
 
 namespace {
@@ -626,38 +639,37 @@ template <int D, int OUT>
 void launch_merge(hipStream_t st, const MxAttnArgs &a) {
   const dim3 grid(a.batch * a.n_nodes, a.c.n_kv), block(a.group * D);   // <= 1024 (group <= 8, d <= 128)
   static_assert(4 * 16 >= kMaxAttnSplits, "every partial is read at once");
-  if (a.n_splits + a.n_own <= 4 * 4) hipLaunchKernelGGL((k_mx_merge<D, 4, OUT>), grid, block, 0, st, a);
+  if (a.n_splits + a.n_own <= 4 * 2) hipLaunchKernelGGL((k_mx_merge<D, 2, OUT>), grid, block, 0, st, a);
+  else if (a.n_splits + a.n_own <= 4 * 4) hipLaunchKernelGGL((k_mx_merge<D, 4, OUT>), grid, block, 0, st, a);
   else if (a.n_splits + a.n_own <= 4 * 8) hipLaunchKernelGGL((k_mx_merge<D, 8, OUT>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((k_mx_merge<D, 16, OUT>), grid, block, 0, st, a);
 }
 
-template <int D, typename T, int NP>
-void launch_parts(hipStream_t st, const MxAttnArgs &a) {
-  const dim3 grid(a.batch * a.c.n_kv, a.n_row_groups, a.n_own + a.n_splits + (a.append ? 1 : 0));
-  if (grid.z == 0) return;   // no key anywhere
-#define TS_MX(KERNEL, THREADS, ...)                                                                                          \
+template <int D, typename T, int NP, int OUT>
+void launch_rows(hipStream_t st, const MxAttnArgs &a) {
+  const int appended = a.append ? 1 : 0;
+  const dim3 grid(a.batch * a.c.n_kv, a.n_row_groups, a.whole ? 1 + appended : a.n_own + a.n_splits + appended);
+#define TS_MX(THREADS, ...)                                                                                          \
   do {                                                                                                              \
-    if (a.c.page_table) hipLaunchKernelGGL((KERNEL<D, __VA_ARGS__, true>), grid, dim3(THREADS), 0, st, a);          \
-    else hipLaunchKernelGGL((KERNEL<D, __VA_ARGS__, false>), grid, dim3(THREADS), 0, st, a);                        \
+    if (a.c.page_table) hipLaunchKernelGGL((k_mx_attn<D, __VA_ARGS__, true>), grid, dim3(THREADS), 0, st, a);          \
+    else hipLaunchKernelGGL((k_mx_attn<D, __VA_ARGS__, false>), grid, dim3(THREADS), 0, st, a);                        \
   } while (0)
-  if (a.form == kMxRows16) TS_MX(k_mx_attn, 256, 1, 1, T, NP);
-  else if (a.form == kMxRows32) TS_MX(k_mx_attn, 256, 2, 1, T, NP);
-  else TS_MX(k_mx_attn, 256, 2, 2, T, NP);
+  if (a.whole) {
+    if (a.form == kMxRows16) TS_MX(512, 1, 1, T, NP, OUT); else TS_MX(512, 2, 1, T, NP, OUT);
+    return;
+  }
+  if (a.form == kMxRows16) TS_MX(256, 1, 1, T, NP, kPartials);
+  else if (a.form == kMxRows32) TS_MX(256, 2, 1, T, NP, kPartials);
+  else TS_MX(256, 2, 2, T, NP, kPartials);
 #undef TS_MX
+  launch_merge<D, OUT>(st, a);
 }
 
 template <int D>
 void launch_d(hipStream_t st, const MxAttnArgs &a) {
-  if (a.out_row == 0) {   // a verification pass
-    launch_parts<D, float, 2>(st, a);
-    launch_merge<D, kOutPanels>(st, a);
-  } else if (a.dtype == TRISPEC_F32) {
-    launch_parts<D, float, 3>(st, a);
-    launch_merge<D, kOutF32>(st, a);
-  } else {
-    launch_parts<D, bf16, 1>(st, a);
-    launch_merge<D, kOutBf16>(st, a);
-  }
+  if (a.out_row == 0) launch_rows<D, float, 2, kOutPanels>(st, a);   // a verification pass
+  else if (a.dtype == TRISPEC_F32) launch_rows<D, float, 3, kOutF32>(st, a);
+  else launch_rows<D, bf16, 1, kOutBf16>(st, a);
 }
 }  // namespace
 

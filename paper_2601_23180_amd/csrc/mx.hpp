@@ -185,9 +185,9 @@ struct MxAttnArgs {
   int32_t chain;
   int32_t batch, n_nodes, n_q_heads, group, head_dim, dtype;
   int32_t append;             // the nodes' K and V go to slots ctx + i
-  int32_t form;               // kMxRows*
+  int32_t whole, form;        // form: kMxRows*
   int32_t n_row_groups, n_splits, n_own;
-  float *part_o, *part_m, *part_l;   // as in AttnArgs; n_own: the draft nodes have a partial of their own, else they are in the last split
+  float *part_o, *part_m, *part_l;   // as in AttnArgs, those of the draft nodes behind those of the splits
   void *out;                  // rows [batch * n_nodes][n_q_heads * d] in dtype, or operand panels
   int64_t out_row;            // elements between rows; 0: operand panels of out_panel 32-row blocks
   size_t out_panel;

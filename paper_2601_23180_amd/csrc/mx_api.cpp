@@ -80,7 +80,7 @@ struct AttendLayout {
 };
 AttendLayout attend_layout(int batch, int n_nodes, int group, int n_kv, int head_dim) {
   // as many splits as the plan makes at most: those of endless contexts, and those of the nodes
-  const MxPlan p = plan_mx(batch, n_kv, group, n_nodes, false, 1l << 30);
+  const MxPlan p = plan_mx(batch, n_kv, group, n_nodes, false, false, 1l << 30);
   const size_t rows = (size_t)batch * n_kv * (p.n_splits + (n_nodes + kMxOwnNodes - 1) / kMxOwnNodes) * group * n_nodes;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   AttendLayout L;
@@ -203,14 +203,14 @@ int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, co
     }
   const AttendLayout L = attend_layout(B, M, group, c->n_kv_heads, D);
   if (!x->workspace || ((uintptr_t)x->workspace & 255) || x->workspace_bytes < L.total) return TRISPEC_EWORKSPACE;
-  const MxPlan p = plan_mx(B, c->n_kv_heads, group, M, own, longest);
+  const MxPlan p = plan_mx(B, c->n_kv_heads, group, M, own, x->dtype == TRISPEC_F32, longest);
   a.c = map_of(c);
   a.q = rows_of(x->q);
   a.k = rows_of(x->k);
   a.v = rows_of(x->v);
   a.batch = B; a.n_nodes = M; a.n_q_heads = x->n_q_heads; a.group = group; a.head_dim = D; a.dtype = x->dtype;
   a.append = x->append;
-  a.form = p.form; a.n_row_groups = p.n_row_groups;
+  a.whole = p.whole; a.form = p.form; a.n_row_groups = p.n_row_groups;
   a.n_splits = p.n_splits; a.n_own = p.n_own;
   char *ws = (char *)x->workspace;
   a.part_o = (float *)(ws + L.o);

@@ -339,6 +339,7 @@ inline AttnPlan plan_attn(int batch, int n_kv, int group, int head_dim, int n_no
 enum { kMxRows16 = 0, kMxRows32, kMxRows64 };   // rows of a workgroup
 constexpr int kMxOwnNodes = 32;                 // draft nodes of a partial
 struct MxPlan {
+  int whole;   // one workgroup takes its rows over everything: no partials
   int form, n_row_groups, n_splits, n_own;   // n_own: partials of the draft nodes, kMxOwnNodes each
 };
 // group * n_nodes query rows per kv head over up to max_keys keys.
@@ -350,7 +351,11 @@ struct MxPlan {
 // 4096 keys, since two workgroups a CU hide each other's latencies.  us, context + merge, once / twice: 60 nodes, 4096 keys 16.0 + 4.0 / 19.4 + 5.1; 128
 // nodes, 8192 keys 32.8 + 5.3 / 33.3 + 6.5; four sequences of 60 nodes and 16384 keys 94.1 + 5.5 / 82.4 + 6.2; eight of one token and 32768 keys 55.5
 // / 46.2 (45.3 for 768 workgroups); one token of one sequence, 32768 keys 10.7 / 11.0, 4096 keys 5.5 / 6.1.
-inline MxPlan plan_mx(int batch, int n_kv, int group, int n_nodes, bool own_nodes, long max_keys) {
+// One workgroup for its rows over everything, up to a length that grows with the workgroups there are: it spares the second launch (4 us on the host, 3 to 4 on the
+// GPU and the gap) and the partials, and leaves CUs idle.  us, whole / context + merge: one token, 1000 keys 8.3 / 5.5 + 3.2, 2000 keys 11.8 / 5.5 + 3.3; 16 nodes, 1000 keys
+// 13.5 / 9.3 + 3.4; eight sequences of one token, 2000 keys 11.4 / 7.0 + 3.5; 60 nodes, 1500 keys 18.3 / 13.5 + 3.9; four sequences of them, 777 keys 18.0 / 20.9 + 6.8, 4096 keys 32.3 / 34.0
+// + 6.9, 8192 keys 55.7 / 55.0 + 6.8; in fp32, one workgroup's time a key being twice as long, 4000 keys 56.9 / 53.8 + 6.8, 4 nodes of one sequence 1000 keys 11.3 / 6.7 + 3.4.
+inline MxPlan plan_mx(int batch, int n_kv, int group, int n_nodes, bool own_nodes, bool f32_rows, long max_keys) {
   const int p_rows = group * n_nodes;
   MxPlan p;
   p.form = p_rows <= 16 ? kMxRows16 : p_rows <= 32 ? kMxRows32 : kMxRows64;
@@ -365,6 +370,9 @@ inline MxPlan plan_mx(int batch, int n_kv, int group, int n_nodes, bool own_node
   if (want < 1) want = 1;
   p.n_splits = (int)((max_keys + 255) / 256);
   if (p.n_splits > want) p.n_splits = want;
+  const int pairs = p_rows <= 16 ? 1 : 2, groups = (p_rows + 16 * pairs - 1) / (16 * pairs);   // as one workgroup takes them whole
+  p.whole = max_keys <= ((pairs == 1 ? 1536 : 1024) + 24l * batch * n_kv * groups) / (f32_rows ? 2 : 1);
+  if (p.whole) { p.form = pairs == 1 ? kMxRows16 : kMxRows32; p.n_row_groups = groups; }
   return p;
 }
 

@@ -230,6 +230,51 @@ def test_scores_that_keep_growing_and_scores_far_apart():
         assert (np.abs(out - want) <= R.tolerance(want, mass, spread, 900 + nodes, 128, False)).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,heads,kv,nodes,ctx,paged,kind", [
+    (128, 4, 2, 1, [1600], False, "chain"),             # 16 rows a workgroup, one sequence
+    (64, 4, 4, 3, [2687, 0, 5, 2688], True, "chain"),   # an empty sequence and a short one among the long
+    (128, 6, 2, 8, [2000, 2049], True, "bush"),         # 32
+    (64, 16, 2, 33, [3000], False, "tree"),             # 64, and two partials of nodes
+    (128, 4, 1, 60, [2433, 77], True, "tree"),
+    (128, 1, 1, 128, [4001], False, "chain"),           # four
+    (64, 8, 8, 2, [3100] * 8, False, "bush"),           # splits for every CU twice, fewer than there are keys for
+])
+def test_attend_beyond_what_one_workgroup_takes(d, heads, kv, nodes, ctx, paged, kind, dtype):
+    attend_case(d, heads, kv, nodes, ctx, dtype, paged, kind, append=nodes % 2 == 0, fused=nodes % 3 != 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nodes", [1, 9])
+def test_attend_on_both_sides_of_the_longest_context_of_one_workgroup(nodes, dtype):
+    for ctx in (600, 640, 1100, 1200, 1500, 1600):
+        attend_case(64, 4, 2, nodes, [ctx], dtype, False, "tree", append=True, seed=ctx)
+
+
+@pytest.mark.parametrize("nodes,heads", [(1, 1), (9, 4), (40, 4)])
+def test_nan_in_a_long_context_reaches_the_rows_that_see_it_and_no_others(nodes, heads):
+    rng = np.random.default_rng(nodes)
+    c = MXCache.empty(2, 2, 64, 4096)
+    k, v = (random_rows(rng, (2, 4000, 2, 64), "f32") for _ in range(2))
+    v[0, 2500, 1, 40] = float("nan")
+    k[1, 3999, 0, 3] = float("inf")
+    mx_append(c, k.cuda(), v.cuda(), [0, 0])
+    q = random_rows(rng, (2, nodes, 2 * heads, 64), "f32").cuda()
+    own_k, own_v = (random_rows(rng, (2, nodes, 2, 64), "f32") for _ in range(2))
+    parents = np.zeros((2, nodes), np.int32)
+    parents[:, 0] = -1
+    if nodes > 2:
+        own_v[0, 1, 0, 7], own_v[0, 2, 0, 8] = float("inf"), float("nan")
+    for length, seen in ((4000, True), (2500, False)):
+        out = torch.isnan(mx_attend(c, [length, length], q, own_k.cuda(), own_v.cuda(), parents=parents)).cpu().unflatten(2, (2, heads))
+        want = torch.zeros(2, nodes, 2, heads, 64, dtype=torch.bool)
+        want[0, :, 1, :, 32:] = seen
+        want[1, :, 0] = seen
+        if nodes > 2:
+            want[0, 2, 0, :, 8] = True
+        assert torch.equal(out, want)
+
+
 @pytest.mark.parametrize("nodes,heads", [(1, 1), (9, 1), (9, 4), (40, 4)])
 def test_nan_reaches_the_rows_that_see_it_and_no_others(nodes, heads):
     rng = np.random.default_rng(nodes)
