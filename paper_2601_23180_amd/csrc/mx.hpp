@@ -100,11 +100,9 @@ __device__ __forceinline__ f32x8 load8(const bf16 *p) {
   const bf16x8 a = *(const bf16x8 *)p;
   return f32x8{(float)a[0], (float)a[1], (float)a[2], (float)a[3], (float)a[4], (float)a[5], (float)a[6], (float)a[7]};
 }
-__device__ __forceinline__ void store8(float *p, bf16x8 v) {
-  *(f32x4 *)p = f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
-  *(f32x4 *)(p + 4) = f32x4{(float)v[4], (float)v[5], (float)v[6], (float)v[7]};
-}
-__device__ __forceinline__ void store8(bf16 *p, bf16x8 v) { *(bf16x8 *)p = v; }
+// 16 bytes of a row, past the L2: four fp32 features or eight in bf16, the first of v
+__device__ __forceinline__ void stream16(float *p, bf16x8 v) { __builtin_nontemporal_store(f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]}, (f32x4 *)p); }
+__device__ __forceinline__ void stream16(bf16 *p, bf16x8 v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4 *)p); }
 
 // Eight features of a block that four lanes side by side hold: their codes, and the block's scale byte.
 __device__ __forceinline__ uint32_t mx_quantise(const f32x8 &x, uint32_t &byte) {
@@ -169,6 +167,7 @@ struct MxReadArgs {
   int64_t k_row, k_seq, v_row, v_seq;
   int32_t head_dim, dtype;
   int32_t start[kMaxBatch], count[kMaxBatch];
+  int32_t first_block;   // of a head's: large ranges go out in several launches
 };
 void launch_mx_append(hipStream_t st, const MxAppendArgs &a, int batch);
 void launch_mx_read(hipStream_t st, const MxReadArgs &a, int batch);
