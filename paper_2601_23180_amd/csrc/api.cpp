@@ -545,7 +545,7 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
   MxAttnArgs mx;
   memset(&mx, 0, sizeof(mx));
   if (kv->held_in_mx) {
-    const MxPlan p = plan_mx(B, c.n_kv_heads, group, n_nodes, true, true, max_keys);
+    const MxPlan p = plan_mx(B, c.n_kv_heads, group, n_nodes, true, true, ctx.v);
     const float *rows_f32 = (const float *)(ws + L.qkv_f32);
     const int64_t seq = (int64_t)n_nodes * nqkv;
     mx.ctx = ctx;
@@ -557,7 +557,8 @@ int trispec_verify(trispec_model *m, trispec_kv *kv, const int32_t *draft_tokens
     mx.dtype = TRISPEC_F32;
     mx.append = 1;
     mx.whole = p.whole; mx.form = p.form; mx.n_row_groups = p.n_row_groups;
-    mx.n_splits = p.n_splits; mx.n_own = p.n_own;
+    mx.n_own = p.n_own; mx.keys = p.keys;
+    mx_split_table(p, B, ctx.v, mx.split0);
     mx.part_o = (float *)(ws + L.attn_o);
     mx.part_m = (float *)(ws + L.attn_m);
     mx.part_l = (float *)(ws + L.attn_l);

@@ -409,8 +409,9 @@ struct OwnSums {
 
 // OwnSums of the 16 rows from first_row on (p_rows and more: none) as a partial.  lds: kPathBytes; every thread of the workgroup comes here.
 template <int D, typename T>
-__device__ __forceinline__ void own_rows(const MxAttnArgs &a, unsigned char *lds, int kvh, int b, int first_row, int n_begin, int n_end, const T *q0, size_t part) {
+__device__ __forceinline__ void own_rows(const MxAttnArgs &a, unsigned char *lds, int kvh, int b, int first_row, int n_begin, int n_end, size_t part) {
   const RootPaths paths(a, lds, b);
+  const T *q0 = (const T *)a.q.p + b * a.q.seq + kvh * a.group * D;
   const OwnRows<T> x(a, kvh, b, D);
   const int p_rows = a.group * x.M, row = first_row + (threadIdx.x & 15);
   if (first_row >= p_rows) return;   // wave-uniform
@@ -423,15 +424,6 @@ __device__ __forceinline__ void own_rows(const MxAttnArgs &a, unsigned char *lds
     a.part_l[part + row] = sums.l;
   }
   sums.store(a.part_o + (part + row) * D);
-}
-
-// an empty split's partial is neutral
-template <int R>
-__device__ __forceinline__ void empty_partial(const MxAttnArgs &a, int row0, int p_rows, size_t part) {
-  for (int r = threadIdx.x; r < min(R, p_rows - row0); r += blockDim.x) {
-    a.part_m[part + row0 + r] = -INFINITY;
-    a.part_l[part + row0 + r] = 0.f;
-  }
 }
 
 // the workgroup behind all others stores the nodes' rows, which nobody reads here
@@ -450,41 +442,40 @@ __device__ __forceinline__ uint32_t low_bits(int left) { return left <= 0 ? 0u :
 // RB blocks of 16 query rows a wavefront; RW wavefronts side by side hold the rows of a workgroup, and KG groups of them take every KG-th run
 // of 32 keys, straight from the cache to registers; the groups' sums meet in LDS at the end.
 //
-// OUT = kPartials: four wavefronts; grid (sequence and kv head, rows, part).  The first n_own parts
-// take the draft nodes, so that the splits behind fill in as those end (four sequences of 60 nodes over 16384 keys: 82 us, 109 with them last); a part behind all
-// others stores the nodes' rows.  Row groups of the same keys land on one XCD wherever sequences times kv heads are a multiple of 8.
+// OUT = kPartials: four wavefronts; grid (kv head, rows, part).  The first parts take the draft nodes, kMxOwnNodes each, so that the splits behind fill in as those end
+// (four sequences of 60 nodes over 16384 keys: 82 us, 109 with them last); then the splits, a.keys keys each whatever sequence they belong to; then a
+// workgroup for each sequence that stores its nodes' rows.  Row groups of the same keys land on one XCD where the kv heads are a multiple of 8.
 // Else: short contexts.  One workgroup of eight wavefronts takes its rows over all keys and nodes and writes their results, which saves the partials' way
 // through memory and the launch behind them; RB of the wavefronts take the draft nodes, 16 rows each.
 template <int D, int RB, int RW, typename T, int NP, int OUT, bool PAGED>
 __global__ __launch_bounds__(OUT == kPartials ? 256 : 512, OUT != kPartials || RB > 1 ? 2 : 3) void k_mx_attn(MxAttnArgs a) {
   constexpr bool kWhole = OUT != kPartials;
-  constexpr int NW = kWhole ? 8 : 4, KG = kWhole ? 8 - RB : 4 / RW, R = 16 * RB * RW, ST = D / 32, NV = D / 64, kUnit = 32 * KG;
+  constexpr int NW = kWhole ? 8 : 4, KG = kWhole ? 8 - RB : 4 / RW, R = 16 * RB * RW, ST = D / 32, NV = D / 64;
   constexpr int LD = D + 4, kSums = kWhole ? KG + 1 : KG;   // rows of sums in LDS: those of the groups, then those of the nodes
   __shared__ __attribute__((aligned(16))) float sums[kSums * R * LD];
   __shared__ float s_m[kSums * R], s_l[kSums * R];
   __shared__ __attribute__((aligned(16))) unsigned char path_lds[kWhole ? kPathBytes : 16];
-  const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv, row0 = blockIdx.y * R, lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x, row0 = blockIdx.y * R, lane = threadIdx.x & 63, ln = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rw = kWhole ? 0 : wave % RW, kg = kWhole ? wave - RB : wave / RW;
-  const int p_rows = a.group * a.n_nodes, split = (int)blockIdx.z - (kWhole ? 0 : a.n_own), n_parts = a.n_splits + a.n_own;
-  const size_t part = (((size_t)b * a.c.n_kv + kvh) * n_parts + (split < 0 ? n_parts + split : split)) * p_rows;
-  const T *q0 = (const T *)a.q.p + b * a.q.seq + kvh * a.group * D;
-  const int ctx = a.ctx.v[b], first_row = row0 + rw * RB * 16;
-  if (split < 0) {   // first of all: the others fill in as these end
-    const int n0 = (-1 - split) * kMxOwnNodes;
-    static_assert(kWhole || sizeof(sums) >= kPathBytes, "the nodes' root paths lie there");
-    return own_rows<D, T>(a, (unsigned char *)sums, kvh, b, wave * 16 < R ? row0 + wave * 16 : p_rows, n0, min(n0 + kMxOwnNodes, a.n_nodes), q0, part);
-  }
-  if (split >= (kWhole ? 1 : a.n_splits)) {
-    if (blockIdx.y == 0) append_rows<D, NW, T>(a, kvh, b);
+  const int n_own = kWhole ? 0 : a.n_own, n_main = kWhole ? a.batch : a.split0[a.batch], p_rows = a.group * a.n_nodes, first_row = row0 + rw * RB * 16;
+  int z = (int)blockIdx.z - n_own * a.batch;
+  if (z >= n_main) {
+    if (blockIdx.y == 0) append_rows<D, NW, T>(a, kvh, z - n_main);
     return;
   }
-  int k_begin = 0, k_end = ctx;
-  if (!kWhole) {   // each sequence's own share
-    const int keys = (ctx + a.n_splits * kUnit - 1) / (a.n_splits * kUnit) * kUnit;
-    k_begin = split * keys;
-    k_end = min(ctx, k_begin + keys);
-    if (k_begin >= k_end) return empty_partial<R>(a, row0, p_rows, part);
+  if (z < 0) {   // first of all: the others fill in as these end
+    const int b = (int)blockIdx.z / a.n_own, n = (int)blockIdx.z - b * a.n_own, n0 = n * kMxOwnNodes;
+    static_assert(kWhole || sizeof(sums) >= kPathBytes, "the nodes' root paths lie there");
+    return own_rows<D, T>(a, (unsigned char *)sums, kvh, b, wave * 16 < R ? row0 + wave * 16 : p_rows, n0, min(n0 + kMxOwnNodes, a.n_nodes),
+                          a.part(a.split0[b + 1] + b * a.n_own + n, kvh));
   }
+  int b = 0;
+  if (kWhole) b = z;
+  else
+    while (z >= a.split0[b + 1]) ++b;
+  const int ctx = a.ctx.v[b], k_begin = kWhole ? 0 : (z - a.split0[b]) * a.keys, k_end = kWhole ? ctx : min(ctx, k_begin + a.keys);
+  const size_t part = a.part(z + b * n_own, kvh);
+  const T *q0 = (const T *)a.q.p + b * a.q.seq + kvh * a.group * D;
   if constexpr (kWhole) {
     const RootPaths paths(a, path_lds, b);
     if (kg < 0) {
@@ -595,9 +586,9 @@ __global__ __launch_bounds__(OUT == kPartials ? 256 : 512, OUT != kPartials || R
 template <int D, int NB, int OUT>
 __global__ __launch_bounds__(1024) void k_mx_merge(MxAttnArgs a) {
   const int r = blockIdx.x, kvh = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int M = a.n_nodes, b = r / M, node = r - b * M, p_rows = a.group * M, n = a.n_splits + a.n_own;
+  const int M = a.n_nodes, b = r / M, node = r - b * M, n = a.split0[b + 1] - a.split0[b] + a.n_own;
   const int al = wave / (D / 64), f = (wave & (D / 64 - 1)) * 64 + (lane & 15) * 4, quarter = lane >> 4;
-  const size_t first = ((size_t)b * a.c.n_kv + kvh) * n * p_rows + al * M + node;
+  const size_t first = a.part(a.split0[b] + b * a.n_own, kvh) + al * M + node, step = a.part(1, 0);
   float m = -INFINITY, l = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
   if (n > 0) {
@@ -605,7 +596,7 @@ __global__ __launch_bounds__(1024) void k_mx_merge(MxAttnArgs a) {
     f32x4 po[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      const size_t idx = first + (size_t)min(quarter + 4 * i, n - 1) * p_rows;
+      const size_t idx = first + min(quarter + 4 * i, n - 1) * step;
       pm[i] = a.part_m[idx];
       pl[i] = a.part_l[idx];
       po[i] = *(const f32x4 *)(a.part_o + idx * D + f);
@@ -616,7 +607,7 @@ __global__ __launch_bounds__(1024) void k_mx_merge(MxAttnArgs a) {
     m = fmaxf(m, __shfl_xor(m, 32, 64));
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      if (quarter + 4 * i >= n || pm[i] == -INFINITY) continue;   // no key in it: its o was never written
+      if (quarter + 4 * i >= n || pm[i] == -INFINITY) continue;
       const float w = __builtin_amdgcn_exp2f((pm[i] - m) * 1.44269504088896f);
       o += po[i] * w;
       l += pl[i] * w;
@@ -639,16 +630,17 @@ template <int D, int OUT>
 void launch_merge(hipStream_t st, const MxAttnArgs &a) {
   const dim3 grid(a.batch * a.n_nodes, a.c.n_kv), block(a.group * D);   // <= 1024 (group <= 8, d <= 128)
   static_assert(4 * 16 >= kMaxAttnSplits, "every partial is read at once");
-  if (a.n_splits + a.n_own <= 4 * 2) hipLaunchKernelGGL((k_mx_merge<D, 2, OUT>), grid, block, 0, st, a);
-  else if (a.n_splits + a.n_own <= 4 * 4) hipLaunchKernelGGL((k_mx_merge<D, 4, OUT>), grid, block, 0, st, a);
-  else if (a.n_splits + a.n_own <= 4 * 8) hipLaunchKernelGGL((k_mx_merge<D, 8, OUT>), grid, block, 0, st, a);
+  int n = 0;
+  for (int b = 0; b < a.batch; ++b) n = max(n, a.split0[b + 1] - a.split0[b] + a.n_own);
+  if (n <= 4 * 2) hipLaunchKernelGGL((k_mx_merge<D, 2, OUT>), grid, block, 0, st, a);
+  else if (n <= 4 * 4) hipLaunchKernelGGL((k_mx_merge<D, 4, OUT>), grid, block, 0, st, a);
+  else if (n <= 4 * 8) hipLaunchKernelGGL((k_mx_merge<D, 8, OUT>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((k_mx_merge<D, 16, OUT>), grid, block, 0, st, a);
 }
 
 template <int D, typename T, int NP, int OUT>
 void launch_rows(hipStream_t st, const MxAttnArgs &a) {
-  const int appended = a.append ? 1 : 0;
-  const dim3 grid(a.batch * a.c.n_kv, a.n_row_groups, a.whole ? 1 + appended : a.n_own + a.n_splits + appended);
+  const dim3 grid(a.c.n_kv, a.n_row_groups, (a.whole ? a.batch : a.split0[a.batch] + a.n_own * a.batch) + (a.append ? a.batch : 0));
 #define TS_MX(THREADS, ...)                                                                                          \
   do {                                                                                                              \
     if (a.c.page_table) hipLaunchKernelGGL((k_mx_attn<D, __VA_ARGS__, true>), grid, dim3(THREADS), 0, st, a);          \

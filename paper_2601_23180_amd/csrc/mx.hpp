@@ -185,8 +185,11 @@ struct MxAttnArgs {
   int32_t batch, n_nodes, n_q_heads, group, head_dim, dtype;
   int32_t append;             // the nodes' K and V go to slots ctx + i
   int32_t whole, form;        // form: kMxRows*
-  int32_t n_row_groups, n_splits, n_own;
-  float *part_o, *part_m, *part_l;   // as in AttnArgs, those of the draft nodes behind those of the splits
+  int32_t n_row_groups, n_own, keys;       // keys of a split; n_own: partials of a sequence's nodes
+  int32_t split0[kMaxBatch + 1];           // splits before those of sequence b
+  float *part_o, *part_m, *part_l;         // as in AttnArgs; a sequence's splits, then its nodes
+  // rows of partial i and kv head h
+  __host__ __device__ size_t part(int i, int h) const { return ((size_t)i * c.n_kv + h) * (group * n_nodes); }
   void *out;                  // rows [batch * n_nodes][n_q_heads * d] in dtype, or operand panels
   int64_t out_row;            // elements between rows; 0: operand panels of out_panel 32-row blocks
   size_t out_panel;

@@ -79,9 +79,7 @@ struct AttendLayout {
   size_t o, m, l, total;
 };
 AttendLayout attend_layout(int batch, int n_nodes, int group, int n_kv, int head_dim) {
-  // as many splits as the plan makes at most: those of endless contexts, and those of the nodes
-  const MxPlan p = plan_mx(batch, n_kv, group, n_nodes, false, false, 1l << 30);
-  const size_t rows = (size_t)batch * n_kv * (p.n_splits + (n_nodes + kMxOwnNodes - 1) / kMxOwnNodes) * group * n_nodes;
+  const size_t rows = mx_max_parts(batch, n_kv, group, n_nodes) * n_kv * group * n_nodes;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   AttendLayout L;
   L.o = 0;
@@ -187,12 +185,10 @@ int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, co
   const int cap = capacity_of(c), group = x->n_q_heads / c->n_kv_heads;
   MxAttnArgs a;
   memset(&a, 0, sizeof(a));
-  int longest = 0;
   for (int b = 0; b < B; ++b) {
     const int n = ctx_len_host[b];
     if (n < 0 || n > cap || (x->append && M > cap - n)) return TRISPEC_ECAPACITY;
     a.ctx.v[b] = n;
-    if (n > longest) longest = n;
   }
   a.chain = tree_parents == nullptr;
   if (tree_parents)
@@ -203,7 +199,7 @@ int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, co
     }
   const AttendLayout L = attend_layout(B, M, group, c->n_kv_heads, D);
   if (!x->workspace || ((uintptr_t)x->workspace & 255) || x->workspace_bytes < L.total) return TRISPEC_EWORKSPACE;
-  const MxPlan p = plan_mx(B, c->n_kv_heads, group, M, own, x->dtype == TRISPEC_F32, longest);
+  const MxPlan p = plan_mx(B, c->n_kv_heads, group, M, own, x->dtype == TRISPEC_F32, a.ctx.v);
   a.c = map_of(c);
   a.q = rows_of(x->q);
   a.k = rows_of(x->k);
@@ -211,7 +207,8 @@ int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, co
   a.batch = B; a.n_nodes = M; a.n_q_heads = x->n_q_heads; a.group = group; a.head_dim = D; a.dtype = x->dtype;
   a.append = x->append;
   a.whole = p.whole; a.form = p.form; a.n_row_groups = p.n_row_groups;
-  a.n_splits = p.n_splits; a.n_own = p.n_own;
+  a.n_own = p.n_own; a.keys = p.keys;
+  mx_split_table(p, B, a.ctx.v, a.split0);
   char *ws = (char *)x->workspace;
   a.part_o = (float *)(ws + L.o);
   a.part_m = (float *)(ws + L.m);

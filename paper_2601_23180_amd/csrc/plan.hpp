@@ -340,40 +340,59 @@ enum { kMxRows16 = 0, kMxRows32, kMxRows64 };   // rows of a workgroup
 constexpr int kMxOwnNodes = 32;                 // draft nodes of a partial
 struct MxPlan {
   int whole;   // one workgroup takes its rows over everything: no partials
-  int form, n_row_groups, n_splits, n_own;   // n_own: partials of the draft nodes, kMxOwnNodes each
+  int form, n_row_groups, n_own;   // n_own: partials of a sequence's draft nodes, kMxOwnNodes each
+  int keys;                        // of a split
 };
 // group * n_nodes query rows per kv head over up to max_keys keys.
 //
 // Rows: one block of 16 a wavefront up to 16 rows, else two, by one or two wavefronts side by side; larger workgroups, also ones that stage converted keys in
 // LDS, are no faster (60 nodes of 4 heads a kv head over 4096 keys, 128 rows a workgroup 18.5 us and 64 rows 15.2, 16384 keys of four sequences 86.3 and 85.7): what
 // bounds the kernel is the conversion beside the products, not the reading.
-// Splits: workgroups for every CU once, the nodes' own among them where they are few, over 256 keys at least; twice where a split would be longer than
-// 4096 keys, since two workgroups a CU hide each other's latencies.  us, context + merge, once / twice: 60 nodes, 4096 keys 16.0 + 4.0 / 19.4 + 5.1; 128
+// Splits: as many keys to each, whatever sequence they belong to; workgroups for every CU once, the nodes' own among them where they are few, over 256
+// keys at least; twice where a split would be longer than 4096 keys, since two workgroups a CU hide each other's latencies.  us, context + merge, once / twice: 60 nodes, 4096 keys 16.0 + 4.0 / 19.4 + 5.1; 128
 // nodes, 8192 keys 32.8 + 5.3 / 33.3 + 6.5; four sequences of 60 nodes and 16384 keys 94.1 + 5.5 / 82.4 + 6.2; eight of one token and 32768 keys 55.5
 // / 46.2 (45.3 for 768 workgroups); one token of one sequence, 32768 keys 10.7 / 11.0, 4096 keys 5.5 / 6.1.
 // One workgroup for its rows over everything, up to a length that grows with the workgroups there are: it spares the second launch (4 us on the host, 3 to 4 on the
 // GPU and the gap) and the partials, and leaves CUs idle.  us, whole / context + merge: one token, 1000 keys 8.3 / 5.5 + 3.2, 2000 keys 11.8 / 5.5 + 3.3; 16 nodes, 1000 keys
 // 13.5 / 9.3 + 3.4; eight sequences of one token, 2000 keys 11.4 / 7.0 + 3.5; 60 nodes, 1500 keys 18.3 / 13.5 + 3.9; four sequences of them, 777 keys 18.0 / 20.9 + 6.8, 4096 keys 32.3 / 34.0
 // + 6.9, 8192 keys 55.7 / 55.0 + 6.8; in fp32, one workgroup's time a key being twice as long, 4000 keys 56.9 / 53.8 + 6.8, 4 nodes of one sequence 1000 keys 11.3 / 6.7 + 3.4.
-inline MxPlan plan_mx(int batch, int n_kv, int group, int n_nodes, bool own_nodes, bool f32_rows, long max_keys) {
+inline int mx_form(int p_rows) { return p_rows <= 16 ? kMxRows16 : p_rows <= 32 ? kMxRows32 : kMxRows64; }
+inline int mx_row_groups(int p_rows) { return (p_rows + (16 << mx_form(p_rows)) - 1) / (16 << mx_form(p_rows)); }
+inline int mx_own_parts(int n_nodes) { return (n_nodes + kMxOwnNodes - 1) / kMxOwnNodes; }
+inline MxPlan plan_mx(int batch, int n_kv, int group, int n_nodes, bool own_nodes, bool f32_rows, const int32_t *ctx) {
   const int p_rows = group * n_nodes;
   MxPlan p;
-  p.form = p_rows <= 16 ? kMxRows16 : p_rows <= 32 ? kMxRows32 : kMxRows64;
-  const int rows = 16 << p.form;
-  p.n_row_groups = (p_rows + rows - 1) / rows;
-  const int per_split = batch * n_kv * p.n_row_groups;
-  p.n_own = own_nodes ? (n_nodes + kMxOwnNodes - 1) / kMxOwnNodes : 0;
-  const int own = p.n_own * per_split;
-  const int room = (long)per_split * max_keys > 256 * 4096l ? 512 : own <= 64 ? 256 - own : 256;
-  int want = room / per_split;
-  if (want > kMaxAttnSplits - p.n_own) want = kMaxAttnSplits - p.n_own;
-  if (want < 1) want = 1;
-  p.n_splits = (int)((max_keys + 255) / 256);
-  if (p.n_splits > want) p.n_splits = want;
+  p.form = mx_form(p_rows);
+  p.n_row_groups = mx_row_groups(p_rows);
+  p.n_own = own_nodes ? mx_own_parts(n_nodes) : 0;
+  long total = 0, longest = 0;
+  for (int b = 0; b < batch; ++b) { total += ctx[b]; if (ctx[b] > longest) longest = ctx[b]; }
+  const long wgs = (long)n_kv * p.n_row_groups, own = p.n_own * batch * wgs;   // workgroups of a split and of the nodes
+  const long room = wgs * total > 256 * 4096l ? 512 : own <= 64 ? 256 - own : 256;
+  auto count = [&](long keys) {
+    long n = 0;
+    for (int b = 0; b < batch; ++b) n += (ctx[b] + keys - 1) / keys;
+    return n;
+  };
+  long keys = (wgs * total + room - 1) / room;
+  if (keys < 256) keys = 256;
+  if (keys * (kMaxAttnSplits - p.n_own) < longest) keys = (longest + kMaxAttnSplits - p.n_own - 1) / (kMaxAttnSplits - p.n_own);
+  const int unit = p.form == kMxRows64 ? 64 : 128;   // a run of every wavefront
+  for (keys = (keys + unit - 1) / unit * unit; keys < longest && count(keys) * wgs > room;) keys += (keys / 16 + unit - 1) / unit * unit;   // sequences end inside a split
+  p.keys = (int)keys;
   const int pairs = p_rows <= 16 ? 1 : 2, groups = (p_rows + 16 * pairs - 1) / (16 * pairs);   // as one workgroup takes them whole
-  p.whole = max_keys <= ((pairs == 1 ? 1536 : 1024) + 24l * batch * n_kv * groups) / (f32_rows ? 2 : 1);
+  p.whole = longest <= ((pairs == 1 ? 1536 : 1024) + 24l * batch * n_kv * groups) / (f32_rows ? 2 : 1);
   if (p.whole) { p.form = pairs == 1 ? kMxRows16 : kMxRows32; p.n_row_groups = groups; }
   return p;
+}
+inline void mx_split_table(const MxPlan &p, int batch, const int32_t *ctx, int32_t *split0) {
+  split0[0] = 0;
+  for (int b = 0; b < batch; ++b) split0[b + 1] = split0[b] + (ctx[b] + p.keys - 1) / p.keys;
+}
+// partials that any plan needs at most
+inline size_t mx_max_parts(int batch, int n_kv, int group, int n_nodes) {
+  const int splits = 512 / (n_kv * mx_row_groups(group * n_nodes));
+  return (splits > batch ? splits : batch) + (size_t)batch * mx_own_parts(n_nodes);
 }
 
 // ---- the plans of one model, made once: the matmuls of a pass depend on its rows only through the kind of panel
