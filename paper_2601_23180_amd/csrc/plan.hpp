@@ -375,6 +375,7 @@ inline MxPlan plan_mx(int batch, int n_kv, int group, int n_nodes, bool own_node
     return n;
   };
   long keys = (wgs * total + room - 1) / room;
+  if (keys > longest) keys = longest;   // a split a sequence
   if (keys < 256) keys = 256;
   if (keys * (kMaxAttnSplits - p.n_own) < longest) keys = (longest + kMaxAttnSplits - p.n_own - 1) / (kMaxAttnSplits - p.n_own);
   const int unit = p.form == kMxRows64 ? 64 : 128;   // a run of every wavefront
