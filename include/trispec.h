@@ -271,8 +271,8 @@ int trispec_mx_read(const trispec_mx_cache *c, const trispec_mx_rows *k, const t
  * and V as they read back, the nodes' own as they are given.  One node is plain decoding.
  *   q             [batch][n_nodes][n_q_heads * head_dim], rotated;  k, v [batch][n_nodes][n_kv_heads * head_dim].  data NULL in both k and v:
  *                 the nodes see the cache alone, and a node that sees no key gets zeros
- *   dtype         of q, k, v and out.  TRISPEC_F32: operands as bf16 high + low pairs; TRISPEC_BF16: exact queries, probabilities
- *                 rounded to bf16.  Sums, maxima and the nodes' own part are fp32 either way
+ *   dtype         of q, k, v and out.  TRISPEC_F32: queries and probabilities as three parts of 8 bits, which keeps fp32 accuracy; TRISPEC_BF16:
+ *                 exact queries, probabilities rounded to bf16.  Sums, maxima and the nodes' own part are fp32 either way
  *   tree_parents  HOST [batch][n_nodes] as in trispec_verify, or NULL: a chain
  *   append        1: the nodes' k and v are also written to slots ctx_len[b] + i (trispec_mx_append, in the same launch)
  *   out           [batch * n_nodes] rows of n_q_heads * head_dim, out_row_stride elements apart
@@ -280,7 +280,7 @@ int trispec_mx_read(const trispec_mx_cache *c, const trispec_mx_rows *k, const t
  *                 captured graphs) need one each
  * ctx_len_host: HOST [batch], read at the call (a captured call replays with the lengths it was captured with).
  * Limits as trispec_verify: batch * n_nodes <= TRISPEC_MAX_ROWS, at most 8 query heads per kv head, n_q_heads / n_kv_heads * n_nodes <= 512.
- * Two launches on `stream`; no allocation, no synchronisation.
+ * One launch on `stream` for short contexts, else two; no allocation, no synchronisation.
  * Errors: those of trispec_mx_append, TRISPEC_ENULL, TRISPEC_ESHAPE, TRISPEC_ENODES, TRISPEC_ETREE, TRISPEC_EWORKSPACE.
  */
 typedef struct {
@@ -299,8 +299,8 @@ int trispec_mx_attend(const trispec_mx_cache *c, const int32_t *ctx_len_host, co
 
 /* A cache object over such memory, for bf16 models: every other call takes it like a bf16 one (trispec_verify, trispec_kv_commit,
  * trispec_ternary_*).  `c` describes layer 0; each array holds the model's n_layers layers one behind another.  A pass quantises the
- * draft nodes' rows as it stores them and attends over the context as it reads back; the nodes of the pass see each other unrounded, as with
- * a bf16 cache.  Errors: TRISPEC_ENULL, TRISPEC_EMISMATCH (n_kv_heads or head_dim are not the model's), TRISPEC_ESHAPE (an fp32
+ * draft nodes' rows as it stores them and attends over the context as it reads back, with queries and probabilities as
+ * bf16 high + low pairs like the pass's other operands; the nodes of the pass see each other unrounded, as with a bf16 cache.  Errors: TRISPEC_ENULL, TRISPEC_EMISMATCH (n_kv_heads or head_dim are not the model's), TRISPEC_ESHAPE (an fp32
  * model), those of trispec_mx_cache_bytes, TRISPEC_EARG (alignment). */
 int trispec_kv_create_mx(const trispec_model *m, const trispec_mx_cache *c, trispec_kv **out);
 

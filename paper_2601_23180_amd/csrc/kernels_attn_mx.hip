@@ -2,14 +2,24 @@
 //
 // For query row r (query head, node) of a kv head: scores s_j = q_r . K_j / sqrt(d) over the context's slots and the row's
 // ancestors, one pass over the keys with the running maximum m and l = sum exp(s_j - m), o = sum exp(s_j - m) V_j, result o / l.
-// Workgroups take a range of keys each and leave (m, l, o); a second launch adds them up in ascending order.
+// Workgroups take a range of keys each and leave (m, l, o); a second launch adds them up in ascending order.  Short contexts take one workgroup for
+// everything, and no second launch.
 //
 // A wavefront takes 32 keys at a time, straight from the cache to registers: a key's codes are so few bytes that sharing a
 // tile through LDS would cost more than converting it once per 16 to 64 query rows.  K Q^T and V^T P^T go through 16 x 16 x 32
 // matrix instructions in the transposed form (a query row per lane, so the softmax state is per lane), and the order of the
 // reduction is chosen so that nothing moves between lanes: score register e of lane (ln, g) is the key 8 g + e of the
 // tile, which is what the second product's operand wants of that lane.  bf16 queries are exact operands and probabilities
-// are rounded to bf16, half a step of the result's own type; fp32 ones go as high part + low part, both.
+// are rounded to bf16, half a step of the result's own type.  fp32 queries and probabilities go as three parts of 8 bits, 24 in all: with two, results were
+// off by 3.7e-6 of their size where fp32 torch is off by 8e-7, with three by 6e-7.  In a verification pass they go in two, 16 bits, like the pass's other operands.
+//
+// What bounds it: for few rows the reading (eight sequences of 32768 keys, 8 kv heads of 128, one token: 285 MB in 46 us, 6.2 TB/s), launch and first data
+// below 4096 keys or so; for many rows the vector ALU, which turns a run of 32 keys into operands by about 100 instructions and weighs 32 rows
+// of it by about 80, next to 34 matrix instructions of 16 cycles (four sequences of 60 nodes and 32 heads over 16384 keys: 82 to 95 us by card, 0.7 to 0.8
+// PFLOP/s).  Tried for that and not better: 64 rows a wavefront, which halves the conversions a row and leaves one wavefront a SIMD (106 us); operands converted once
+// for all rows in LDS (86 to 106); the masking of a split's end as a loop of its own (the same); each operand converted in front of its product instead of
+// all at once (2 to 8 % slower).  Joining the partials in the last workgroup of a row instead of by a second launch: 10.6 + 3.8 us became 19 to 22, since what other
+// workgroups wrote has to be read past the L2 in a chain of stamp, maxima and sums.
 #include <float.h>
 
 #include "mx.hpp"

@@ -230,6 +230,25 @@ def test_scores_that_keep_growing_and_scores_far_apart():
         assert (np.abs(out - want) <= R.tolerance(want, mass, spread, 900 + nodes, 128, False)).all()
 
 
+@pytest.mark.parametrize("d,heads,kv,nodes,ctx", [(128, 4, 2, 1, 100), (64, 4, 1, 9, 700), (128, 4, 2, 9, 2500), (128, 8, 2, 60, 3000), (64, 2, 2, 40, 0)])
+def test_fp32_rows_lose_nothing_to_the_matrix_instructions_type(d, heads, kv, nodes, ctx):
+    """fp32 operands go in three parts of 8 bits, 24 in all, so a score is the fp32 sum of 3 d exact products: off by (3 d + 8) 2^-24 of
+    sum |q| |k| / sqrt(d), the scale, the maximum and the parts' cut at the end among the 8.  A weight is off by that twice (numerator, and sum of weights), by
+    its own cut and exponential, 4 of 2^-24, twice as well, and by the sums' (3 n + 64) 2^-24; a factor of 2 for second-order terms."""
+    rng = np.random.default_rng([nodes, ctx])
+    c = MXCache.empty(1, kv, d, 4096)
+    k_ctx, v_ctx = (random_rows(rng, (1, max(ctx, 1), kv, d), "f32") for _ in range(2))
+    mx_append(c, k_ctx.cuda(), v_ctx.cuda(), [0], [ctx])
+    x = random_rows(rng, (1, nodes, heads + 2 * kv, d), "f32")
+    q, k, v = x[:, :, :heads], x[:, :, heads:heads + kv], x[:, :, heads + kv:]
+    y = x.cuda()
+    out = mx_attend(c, [ctx], y[:, :, :heads], y[:, :, heads:heads + kv], y[:, :, heads + kv:])[0].double().cpu().numpy()
+    kb, vb = (R.rounded(t[0, :ctx].double().numpy()) for t in (k_ctx, v_ctx))
+    want, mass, spread = R.attend(q[0].double().numpy(), kb, vb, k[0].double().numpy(), v[0].double().numpy(), tree(rng, nodes, "chain"))
+    weight = 2 * (3 * d + 8) * 2.0 ** -24 * spread + (2 * 4 + 3 * (ctx + nodes) + 64) * 2.0 ** -24
+    assert (np.abs(out - want) <= 2 * weight * mass + 2.0 ** -24 * np.abs(want)).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("d,heads,kv,nodes,ctx,paged,kind", [
     (128, 4, 2, 1, [1600], False, "chain"),             # 16 rows a workgroup, one sequence
