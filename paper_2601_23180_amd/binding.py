@@ -512,12 +512,13 @@ def _mx_dtype(t: torch.dtype) -> int:
 def _elsewhere(cache: MXCache, stream) -> bool:
     """Whether an operator is to run on another stream, or device, than the current one."""
     if stream is None:
-        return cache.index != torch.cuda.current_device()
+        return cache.index != _current_device()
     if stream.device != cache.device:
         raise ValueError(f"a stream on {cache.device} is wanted")
     return True
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 # the current stream of a device as a number, 30 times as fast as torch.cuda.current_stream().cuda_stream
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
@@ -550,9 +551,11 @@ def mx_read(cache: MXCache, start: Sequence[int], n: int, dtype: torch.dtype = t
         with torch.cuda.device(cache.device), torch.cuda.stream(stream):   # what is allocated here belongs to that stream
             return mx_read(cache, start, n, dtype)
     d = _mx_dtype(dtype)
-    k, v = torch.empty((2, cache.batch, n, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=cache.device).unbind(0)
+    row = cache.n_kv_heads * cache.head_dim
+    shape, strides = (cache.batch, n, cache.n_kv_heads, cache.head_dim), (n * row, row, cache.head_dim, 1)
+    k = torch.empty_strided(shape, strides, dtype=dtype, device=cache.device)   # 0.5 us less than torch.empty
+    v = torch.empty_strided(shape, strides, dtype=dtype, device=cache.device)
     if n > 0:
-        row = cache.n_kv_heads * cache.head_dim
         rc = lib().trispec_mx_read(cache.ref, _pack_rows(k.data_ptr(), row, n * row), _pack_rows(v.data_ptr(), row, n * row), d, cache.ints(start),
                                    cache.ints((n,) * cache.batch), _raw_stream(cache.index))
         if rc:
@@ -586,14 +589,15 @@ def mx_attend(cache: MXCache, ctx_len: Sequence[int], q: torch.Tensor, k: Option
         parents = (parents if parents.dtype == np.int32 else parents.astype(np.int32)).tobytes()
     need = cache.workspace_bytes(m, heads)
     if workspace is None:
-        workspace, have = torch.empty(need, dtype=torch.uint8, device=device), need
+        workspace, have = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=device), need
     elif workspace.device != device or not workspace.is_contiguous():
         raise ValueError("mx_attend: a contiguous workspace on the cache's device is wanted")
     else:
         have = workspace.numel() * workspace.element_size()
-    out = torch.empty(shape, dtype=dtype, device=device)
+    row = heads * cache.head_dim
+    out = torch.empty_strided(shape, (m * row, row, cache.head_dim, 1), dtype=dtype, device=device)
     rc = lib().trispec_mx_attend(cache.ref, cache.ints(ctx_len), parents, _pack_attend(
-        *rq, *rk, *rv, _mx_dtype(dtype), m, heads, 1 if append else 0, out.data_ptr(), heads * cache.head_dim, workspace.data_ptr(), have,
+        *rq, *rk, *rv, _mx_dtype(dtype), m, heads, 1 if append else 0, out.data_ptr(), row, workspace.data_ptr(), have,
         _raw_stream(cache.index)))
     if rc:
         check(rc)
