@@ -14,10 +14,11 @@
 // off by 3.7e-6 of their size where fp32 torch is off by 8e-7, with three by 6e-7.  In a verification pass they go in two, 16 bits, like the pass's other operands.
 //
 // What bounds it: for few rows the reading (eight sequences of 32768 keys, 8 kv heads of 128, one token: 285 MB in 46 us, 6.2 TB/s), launch and first data
-// below 4096 keys or so; for many rows the vector ALU, which turns a run of 32 keys into operands by about 100 instructions and weighs 32 rows
-// of it by about 80, next to 34 matrix instructions of 16 cycles (four sequences of 60 nodes and 32 heads over 16384 keys: 82 to 95 us by card, 0.7 to 0.8
-// PFLOP/s).  Tried for that and not better: 64 rows a wavefront, which halves the conversions a row and leaves one wavefront a SIMD (106 us); operands converted once
-// for all rows in LDS (86 to 106); the masking of a split's end as a loop of its own (the same); each operand converted in front of its product instead of
+// below 4096 keys or so; for many rows no one part (four sequences of 60 nodes and 32 heads over 16384 keys: 82 to 95 us by card, 0.7 to 0.8 PFLOP/s): a run of 32 keys
+// under 32 rows is 34 matrix instructions of 16 cycles, about 110 vector instructions of conversion and 60 of softmax, a third of them exponentials.  Timed without the draft
+// nodes, 88 us; with the keys' conversion left out 88, the values' 87, both 77, the exponentials 84, the loads 79.  Tried for that and not better: three wavefronts a SIMD (12
+// registers spilled: 101); 64 rows a wavefront, which halves the conversions a row and leaves one wavefront a SIMD (106); operands converted once
+// for all rows in LDS (86 to 106); each operand converted in front of its product instead of
 // all at once (2 to 8 % slower).  Joining the partials in the last workgroup of a row instead of by a second launch: 10.6 + 3.8 us became 19 to 22, since what other
 // workgroups wrote has to be read past the L2 in a chain of stamp, maxima and sums.
 #include <float.h>
@@ -498,9 +499,10 @@ __global__ __launch_bounds__(OUT == kPartials ? 256 : 512, OUT != kPartials || R
         own.store(sums + at * LD);
       } else if (g == 0) {
         s_m[at] = -INFINITY;
+        s_l[at] = 0.f;
       }
     } else if (kg * 32 >= ctx) {   // no run
-      for (int i = lane; i < R; i += 64) s_m[kg * R + i] = -INFINITY;
+      for (int i = lane; i < R; i += 64) { s_m[kg * R + i] = -INFINITY; s_l[kg * R + i] = 0.f; }
     }
   }
 
@@ -559,20 +561,14 @@ __global__ __launch_bounds__(OUT == kPartials ? 256 : 512, OUT != kPartials || R
 #pragma unroll
     for (int k = 1; k < kSums; ++k) m = fmaxf(m, s_m[k * R + r]);
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    if constexpr (kSums == 1) {
-      l = s_l[r];
-      o = *(const f32x4 *)(sums + r * LD + f);
-    } else {
 #pragma unroll
-      for (int k = 0; k < kSums; ++k) {
-        // nothing there (or scores of -infinity, which weigh nothing)
-        const float mk = s_m[k * R + r], lk = s_l[k * R + r], w = __builtin_amdgcn_exp2f(mk - m);
-        const f32x4 ok = *(const f32x4 *)(sums + (k * R + r) * LD + f);
-        const bool some = mk != -INFINITY;
-        l += some ? lk * w : 0.f;
+    for (int k = 0; k < kSums; ++k) {
+      const float mk = s_m[k * R + r], lk = s_l[k * R + r], w = __builtin_amdgcn_exp2f(mk - m);
+      const f32x4 ok = *(const f32x4 *)(sums + (k * R + r) * LD + f);
+      const bool some = mk != -INFINITY || lk != 0.f;   // else no key, or scores of -infinity alone; NaN scores leave no maximum but a NaN sum
+      l += some ? lk * w : 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += some ? ok[e] * w : 0.f;
-      }
+      for (int e = 0; e < 4; ++e) o[e] += some ? ok[e] * w : 0.f;
     }
     if constexpr (kWhole) {
       const int al = (row0 + r) / a.n_nodes, node = row0 + r - al * a.n_nodes;

@@ -323,6 +323,22 @@ def test_nan_reaches_the_rows_that_see_it_and_no_others(nodes, heads):
     assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("ctx,first,count", [(1, 0, 1), (40, 0, 40), (300, 32, 32), (300, 0, 300), (3000, 0, 3000), (3000, 1024, 600)])
+@pytest.mark.parametrize("nodes", [1, 9])
+def test_keys_that_are_all_nan_reach_every_row(nodes, ctx, first, count, dtype):
+    """Runs, and whole contexts, without a score that is a number."""
+    rng = np.random.default_rng(ctx)
+    c = MXCache.empty(1, 2, 64, 4096)
+    k, v = (random_rows(rng, (1, ctx, 2, 64), "f32") for _ in range(2))
+    k[0, first:first + count, 0] = float("nan")
+    mx_append(c, k.cuda(), v.cuda(), [0])
+    q, own = random_rows(rng, (1, nodes, 4, 64), dtype).cuda(), random_rows(rng, (1, nodes, 2, 64), dtype).cuda()
+    for mine in (own, None):
+        out = torch.isnan(mx_attend(c, [ctx], q, mine, mine)).cpu()
+        assert out[:, :, :2].all() and not out[:, :, 2:].any()
+
+
 def test_page_ids_outside_the_pool_are_clamped():
     table = torch.tensor([[-5, 1000]], dtype=torch.int32, device="cuda")
     c = MXCache.empty(1, 1, 64, 0, table, 3)
