@@ -13,7 +13,8 @@
 // are rounded to bf16, half a step of the result's own type.  fp32 queries and probabilities go as three parts of 8 bits, 24 in all: with two, results were
 // off by 3.7e-6 of their size where fp32 torch is off by 8e-7, with three by 6e-7.  In a verification pass they go in two, 16 bits, like the pass's other operands.
 //
-// What bounds it: for few rows the reading (eight sequences of 32768 keys, 8 kv heads of 128, one token: 285 MB in 46 us, 6.2 TB/s), launch and first data
+// What bounds it: for few rows the reading (eight sequences of up to 32768 keys, 8 kv heads of 128, one token: 214 MB, cold, in 44 to 46 us; 285 MB in 46 where part of it lies in
+// the last-level cache), launch and first data
 // below 4096 keys or so; for many rows no one part (four sequences of 60 nodes and 32 heads over 16384 keys: 82 to 95 us by card, 0.7 to 0.8 PFLOP/s): a run of 32 keys
 // under 32 rows is 34 matrix instructions of 16 cycles, about 110 vector instructions of conversion and 60 of softmax, a third of them exponentials.  Timed without the draft
 // nodes, 88 us; with the keys' conversion left out 88, the values' 87, both 77, the exponentials 84, the loads 79.  Tried for that and not better: three wavefronts a SIMD (12

@@ -126,6 +126,27 @@ def test_a_cache_beyond_32_bits():
     assert (np.abs(out[:7] - want) <= 10 * 2.0 ** -24 * np.abs(want)).all()
 
 
+def test_a_range_that_takes_more_than_one_launch():
+    """2^23 workgroups and some, over two pages that a table repeats."""
+    from paper_2601_23180_amd import binding as B
+    n, heads, row = (1 << 18) + 40, 1024, 1024 * 64
+    table = (torch.arange(1025, dtype=torch.int32) % 2)[None].cuda()
+    c = MXCache.empty(1, heads, 64, 0, table, 2)
+    rows = random_rows(np.random.default_rng(5), (1, 512, heads, 64), "bf16").cuda()
+    mx_append(c, rows, rows, [0])
+    want = mx_read(c, [0], 512)[0][0]
+    out = torch.empty((n, heads, 64), dtype=torch.bfloat16, device="cuda")
+    out[-512:] = -1
+    B.check(B.lib().trispec_mx_read(c.ref, B._pack_rows(out.data_ptr(), row, n * row), None, B.TRISPEC_BF16, c.ints([0]), c.ints([n]),
+                                    torch.cuda.current_stream().cuda_stream))
+    for first in (0, 512 * 300 + 7, (1 << 18) - 30, n - 100):
+        for i in range(first, first + 100, 9):
+            if i < n:
+                assert torch.equal(out[i], want[i % 512]), i
+    del out
+    torch.cuda.empty_cache()
+
+
 def tree(rng, m, kind):
     if kind == "chain":
         return np.arange(-1, m - 1, dtype=np.int32)
